@@ -65,6 +65,10 @@ extern "C" {
 #define KVCRUSH_BF16  0
 #define KVCRUSH_FP16  1
 #define KVCRUSH_FP32  2
+/* element types of a quantised cache (kvcrush_quantize) */
+#define KVCRUSH_INT8  3
+#define KVCRUSH_E4M3  4
+#define KVCRUSH_INT4  5
 
 /* stages, for kvcrush_workspace_size */
 #define KVCRUSH_STAGE_SCORE      0
@@ -366,6 +370,135 @@ int kvcrush_kmeans_select(const kvcrush_problem_t* problem, const float* scores_
 int kvcrush_signature_static(const kvcrush_problem_t* problem, const float* scores_dev,
                              const int32_t* sig_keep_dev, uint32_t* sigs_dev,
                              int32_t* status_dev, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * The reduced cache in 8 or 4 bits, and the attention that reads it
+ *
+ * A quantised cache is two token-major arrays: codes, described by a kvcrush_tensor_t of type KVCRUSH_INT8,
+ * KVCRUSH_E4M3 (one byte a channel) or KVCRUSH_INT4 (two channels a byte, channel 2i in the low four bits), and
+ * one float32 scale (INT4: a scale and a zero, side by side) for every row, that is for every token and KV head:
+ *   INT8   value = scale * code             code in -127 .. 127, scale = max|x| * (1/127)
+ *   E4M3   value = scale * code             code an 8-bit float (4 exponent, 3 mantissa bits), scale = max|x| * (1/448)
+ *   INT4   value = zero + scale * code      code in 0 .. 15, zero = min x, scale = (max x - min x) * (1/15)
+ * Codes are the quotient x / scale (INT4: (x - zero) / scale), rounded to the nearest code, ties to even.  A scale below
+ * the smallest normal float32 is stored as 0 and so are the row's codes.  A row that holds an infinity or a NaN (INT4:
+ * also one whose span overflows) gets NaN as its scale and zero, and codes 0: it reads back as NaN throughout.
+ * Strides of INT4 codes count channels; like every other stride they must come to multiples of 16 bytes.
+ */
+typedef struct kvcrush_scales {
+  float* ptr_dev;                 /* 4-byte aligned; INT4: 8-byte aligned */
+  int64_t stride_layer;           /* in floats; INT4: even */
+  int64_t stride_token;
+  int64_t stride_head;
+} kvcrush_scales_t;
+
+/*
+ * Stage 4 for a cache of few bits: rows are quantised as they are written.  kvcrush_dequantize is the way back.  Both
+ * move, for K and for V and for every KV head,
+ *   in row   in_begin[l][s] + (idx ? idx[i] : i - cu_kept[seg])          seg = l*n_seqs + s,
+ *   to row   out_begin[l][s] + i - cu_kept[seg]                          cu_kept[seg] <= i < cu_kept[seg + 1]
+ * of layer l, so that one call gathers kept tokens into the reduced cache (as kvcrush_compact does), appends the rows
+ * of new tokens, or reads any part of a cache back.
+ *   cu_kept_dev    [n_layers*n_seqs + 1] int32; NULL: every token of every sequence (idx_dev is NULL too, total_kept is
+ *                  ignored)
+ *   idx_dev        row numbers; NULL: consecutive rows
+ *   total_kept     >= cu_kept[n_layers*n_seqs] (host value, for grid sizing)
+ *   in_begin_dev   [n_layers][n_seqs] int32; NULL: cu_seqlens[s]
+ *   out_begin_dev  [n_layers][n_seqs] int32; NULL: cu_kept[seg] - cu_kept[l*n_seqs] (cu_seqlens[s] without a list)
+ *   K, V           inputs and outputs as for kvcrush_compact; V (with its scales and output) may be NULL.  Type of the
+ *                  16- or 32-bit side: BF16, FP16 or FP32.  head_dim <= 256, a multiple of 8; INT8 and E4M3: of 16,
+ *                  INT4: of 32
+ * Rows that the lists do not name are left as they were.  Two rows written to one place are a race.
+ */
+int kvcrush_quantize(const kvcrush_problem_t* problem, const kvcrush_tensor_t* K, const kvcrush_tensor_t* V,
+                     const int32_t* cu_kept_dev, const int32_t* idx_dev, int64_t total_kept,
+                     const int32_t* in_begin_dev, const int32_t* out_begin_dev,
+                     const kvcrush_tensor_t* K_codes, const kvcrush_scales_t* K_scales,
+                     const kvcrush_tensor_t* V_codes, const kvcrush_scales_t* V_scales,
+                     int32_t* status_dev, void* stream);
+int kvcrush_dequantize(const kvcrush_problem_t* problem, const kvcrush_tensor_t* K_codes, const kvcrush_scales_t* K_scales,
+                       const kvcrush_tensor_t* V_codes, const kvcrush_scales_t* V_scales,
+                       const int32_t* cu_kept_dev, const int32_t* idx_dev, int64_t total_kept,
+                       const int32_t* in_begin_dev, const int32_t* out_begin_dev,
+                       const kvcrush_tensor_t* K, const kvcrush_tensor_t* V, int32_t* status_dev, void* stream);
+
+/* The new tokens of every sequence: sequence s owns tokens [cu_new[s], cu_new[s+1]) of the packed new-token axis. */
+typedef struct kvcrush_new_tokens {
+  int32_t total_new;              /* cu_new[n_seqs] */
+  int32_t max_new;                /* most new tokens of a sequence, <= 1024 */
+  int32_t mask_words;             /* words of a mask row, 32 * mask_words >= max_new; 0 without a mask */
+  int32_t reserved;               /* set to 0 */
+  const int32_t* cu_new_host;     /* [n_seqs+1] ascending from 0; HOST copy */
+  const int32_t* cu_new_dev;      /* the same array in device memory */
+  const uint32_t* mask_dev;       /* optional [total_new][mask_words]: bit j of token i's row: i attends to token j of
+                                     its own sequence; later bits are ignored.  NULL: tokens j <= i */
+} kvcrush_new_tokens_t;
+
+/*
+ * Attention of new tokens over a cache: a generated token for each sequence, or a tree of drafted ones.
+ *   o[l][i][h] = sum_t softmax_t(q[l][i][h] . k[l][t][h div G] * softmax_scale) v[l][t][h div G]
+ * over the rows t that new token i sees:
+ *   with K_new     every cached row of its sequence, and the new tokens that its mask row names;
+ *   without        the new tokens are the last rows of the cache already (n of them, L rows in all): token j of the
+ *                  sequence sees its own row and those before, rows [0, L - n + 1 + j); no mask may be given
+ *   problem        the cache: n_layers, heads, softmax_scale, sequences.  total_tokens is the number of rows a layer holds;
+ *                  causal and query_window are ignored
+ *   row_begin_dev, optional [n_layers][n_seqs] int32, both or none: where each sequence's rows start in its layer, and how
+ *   row_count_dev  many there are (reduced caches differ from layer to layer; a cache grows while it is used).  Counts are
+ *                  taken up to max_seqlen and up to the layer's end.  NULL: cu_seqlens
+ *   Q, K_new, V_new, O   [n_layers][total_new][heads][head_dim]; Q, K_new, V_new and O are of one type, BF16, FP16 or
+ *                  FP32; K_new and V_new both or none
+ *   K, V           the cache: of Q's type (scales NULL) or quantised, both in the same type
+ *   lse_out_dev    optional out [n_layers][n_q_heads][total_new] float32, natural log
+ * head_dim <= 256, a multiple of 8 (quantised caches: see kvcrush_quantize).  Without new tokens (total_new 0) nothing is
+ * done; K and V of a problem without rows may have NULL pointers.  A token that sees no row, or whose logits are
+ * all -inf, gets zeros and a log-sum-exp of -inf.  Rows that a token does not see have no influence on its output,
+ * whatever they hold.  Logits, softmax statistics and sums are float32; the weights are rounded to the 16-bit type that
+ * they are multiplied in (FP32: not at all).  Results do not depend on what else runs, nor on the order of the blocks.
+ */
+int kvcrush_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* new_tokens, const kvcrush_tensor_t* Q,
+                   const kvcrush_tensor_t* K, const kvcrush_scales_t* K_scales,
+                   const kvcrush_tensor_t* V, const kvcrush_scales_t* V_scales,
+                   const kvcrush_tensor_t* K_new, const kvcrush_tensor_t* V_new,
+                   const int32_t* row_begin_dev, const int32_t* row_count_dev,
+                   const kvcrush_tensor_t* O, float* lse_out_dev, int32_t* status_dev, void* stream);
+
+/*
+ * Bounds of the keys of every page: the least and the largest value of each channel, for kvcrush_attend_pages.
+ *   lo[l][s * max_pages + p][h][c], hi[..] = min, max over the rows of page p of sequence s of k[l][.][h][c]
+ * with max_pages = ceil(max_seqlen / page_size); a NaN in a channel makes both its bounds NaN.  Rows of pages that a
+ * sequence does not have are left as they were.
+ *   K            the keys in BF16, FP16 or FP32 (before they are quantised); lo, hi: the same type
+ *   page_size    a multiple of 8, up to 1024
+ *   recent_pages 0: all pages; n > 0: only the last n of every sequence (what a cache needs when it has grown)
+ *   row_begin_dev, row_count_dev   as for kvcrush_attend
+ */
+int kvcrush_page_bounds(const kvcrush_problem_t* problem, const kvcrush_tensor_t* K, int page_size, int recent_pages,
+                        const int32_t* row_begin_dev, const int32_t* row_count_dev,
+                        const kvcrush_tensor_t* lo, const kvcrush_tensor_t* hi, int32_t* status_dev, void* stream);
+
+/*
+ * Attention of new tokens over the pages that look best to them: nothing is evicted, but a token reads only `budget`
+ * pages of its sequence for each KV head.  The new tokens are the last rows of the cache (kvcrush_attend without
+ * K_new); a token that sees L rows chooses among its ceil(L / page_size) pages:
+ *   score(p) = sum over channels c of hi[p][c] * a[c] + lo[p][c] * b[c],
+ *   a[c], b[c] = the sums, over the query heads of the KV head's group, of the positive and of the negative q[h][c]
+ * (the heads' upper bounds on q . k, added up; float64; terms with a = 0 or b = 0 are left out, a NaN counts as +inf).
+ * The first keep_initial and the last keep_recent pages come before all others (lower page first), then pages by
+ * score (ties: lower page); the first `budget` of this order are attended to, or all of them if there are fewer.
+ *   lo, hi         as kvcrush_page_bounds writes them, of Q's type; total rows n_seqs * max_pages
+ *   budget         >= 1
+ *   page_idx_dev   optional out [n_layers][total_new][n_kv_heads][budget] int32: the pages, ascending, then -1
+ *   n_pages_dev    optional out [n_layers][total_new][n_kv_heads] int32: how many there are
+ * At most 8192 pages a sequence.  Other arguments as for kvcrush_attend (mask_dev must be NULL).
+ */
+int kvcrush_attend_pages(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* new_tokens, const kvcrush_tensor_t* Q,
+                         const kvcrush_tensor_t* K, const kvcrush_scales_t* K_scales,
+                         const kvcrush_tensor_t* V, const kvcrush_scales_t* V_scales,
+                         int page_size, const kvcrush_tensor_t* lo, const kvcrush_tensor_t* hi, int budget,
+                         int keep_initial, int keep_recent, const int32_t* row_begin_dev, const int32_t* row_count_dev,
+                         int32_t* page_idx_dev, int32_t* n_pages_dev,
+                         const kvcrush_tensor_t* O, float* lse_out_dev, int32_t* status_dev, void* stream);
 
 /* Text for a return code. */
 const char* kvcrush_strerror(int code);

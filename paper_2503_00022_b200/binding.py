@@ -22,6 +22,7 @@ ERR_STATIC_LIMIT = -6
 STATIC_THETA_MAX = 65536
 DEV_OK, DEV_TIMEOUT, DEV_BUDGET = 0, 1, 2
 BF16, FP16, FP32 = 0, 1, 2
+INT8, E4M3, INT4 = 3, 4, 5
 STAGE_SCORE, STAGE_SIGNATURE, STAGE_SELECT, STAGE_COMPACT = 0, 1, 2, 3
 ANCHOR_ALTERNATE, ANCHOR_MEAN, ANCHOR_EXPLICIT = 0, 1, 2
 SCORE_AUTO, SCORE_SIMT, SCORE_TENSOR = 0, 1, 2
@@ -29,7 +30,8 @@ SCORE_AUTO, SCORE_SIMT, SCORE_TENSOR = 0, 1, 2
 EXPORTS = ("kvcrush_workspace_size", "kvcrush_score", "kvcrush_signature", "kvcrush_select",
            "kvcrush_compact", "kvcrush_strerror", "kvcrush_version", "kvcrush_signature_static",
            "kvcrush_pool_scores", "kvcrush_select_pages", "kvcrush_compact_pages", "kvcrush_score_decode",
-           "kvcrush_compact_scores", "kvcrush_kmeans_workspace_size", "kvcrush_kmeans_select")
+           "kvcrush_compact_scores", "kvcrush_kmeans_workspace_size", "kvcrush_kmeans_select", "kvcrush_quantize",
+           "kvcrush_dequantize", "kvcrush_attend", "kvcrush_page_bounds", "kvcrush_attend_pages")
 
 
 class ProblemStruct(ctypes.Structure):
@@ -45,6 +47,21 @@ class TensorStruct(ctypes.Structure):
     _fields_ = [
         ("ptr_dev", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
         ("stride_layer", ctypes.c_int64), ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+    ]
+
+
+class ScalesStruct(ctypes.Structure):
+    _fields_ = [
+        ("ptr_dev", ctypes.c_void_p), ("stride_layer", ctypes.c_int64), ("stride_token", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+    ]
+
+
+class NewTokensStruct(ctypes.Structure):
+    _fields_ = [
+        ("total_new", ctypes.c_int32), ("max_new", ctypes.c_int32), ("mask_words", ctypes.c_int32),
+        ("reserved", ctypes.c_int32), ("cu_new_host", ctypes.c_void_p), ("cu_new_dev", ctypes.c_void_p),
+        ("mask_dev", ctypes.c_void_p),
     ]
 
 
@@ -80,6 +97,12 @@ def lib() -> ctypes.CDLL:
         L.kvcrush_select_pages.argtypes = [P, vp, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp, vp]
         L.kvcrush_compact_pages.argtypes = [P, T, T, i32, vp, vp, i64, T, T, vp, vp]
         L.kvcrush_signature_static.argtypes = [P, vp, vp, vp, vp, vp]
+        C, N = ctypes.POINTER(ScalesStruct), ctypes.POINTER(NewTokensStruct)
+        L.kvcrush_quantize.argtypes = [P, T, T, vp, vp, i64, vp, vp, T, C, T, C, vp, vp]
+        L.kvcrush_dequantize.argtypes = [P, T, C, T, C, vp, vp, i64, vp, vp, T, T, vp, vp]
+        L.kvcrush_attend.argtypes = [P, N, T, T, C, T, C, T, T, vp, vp, T, vp, vp, vp]
+        L.kvcrush_page_bounds.argtypes = [P, T, i32, i32, vp, vp, T, T, vp, vp]
+        L.kvcrush_attend_pages.argtypes = [P, N, T, T, C, T, C, i32, T, T, i32, i32, i32, vp, vp, vp, vp, T, vp, vp, vp]
         L.kvcrush_strerror.argtypes = [i32]
         L.kvcrush_strerror.restype = ctypes.c_char_p
         L.kvcrush_version.argtypes = []
@@ -163,6 +186,62 @@ def tensor_struct(t) -> TensorStruct:
     strides = t.stride()
     assert len(strides) == 4 and strides[3] == 1, "expected [layers, tokens, heads, D] with contiguous D"
     return TensorStruct(t.data_ptr(), dtype_code(t.dtype), 0, *strides[:3])
+
+
+class QuantTensor:
+    """K or V of a quantised cache: codes [layers, rows, heads, D bytes (INT4: D/2)] (uint8) and float32 scales
+    [layers, rows, heads] (INT4: [layers, rows, heads, 2], scale and zero), both with any strides but along the last axis.
+    Owns nothing but the two tensors and their descriptors."""
+
+    def __init__(self, codes, scales, format: int):
+        import torch
+        assert codes.element_size() == 1 and codes.dim() == 4 and codes.stride(3) == 1, "expected [layers, rows, heads, bytes]"
+        assert scales.dtype == torch.float32 and scales.dim() == (4 if format == INT4 else 3)
+        assert scales.shape[:3] == codes.shape[:3] and (format != INT4 or (scales.shape[3] == 2 and scales.stride(3) == 1))
+        self.codes, self.scales, self.format = codes, scales, int(format)
+        per_byte = 2 if format == INT4 else 1
+        self.head_dim = int(codes.shape[3]) * per_byte
+        self.struct = TensorStruct(codes.data_ptr(), self.format, 0, *(per_byte * x for x in codes.stride()[:3]))
+        self.scales_struct = ScalesStruct(scales.data_ptr(), *scales.stride()[:3])
+
+    @classmethod
+    def empty(cls, n_layers: int, rows: int, n_heads: int, head_dim: int, format: int, device="cuda:0") -> "QuantTensor":
+        """An uninitialised cache; the scales of a head lie side by side, as attention reads them."""
+        import torch
+        int4 = format == INT4
+        codes = torch.empty((n_layers, rows, n_heads, head_dim // 2 if int4 else head_dim), dtype=torch.uint8, device=device)
+        scales = torch.empty((n_layers, n_heads, rows) + ((2,) if int4 else ()), dtype=torch.float32, device=device)
+        return cls(codes, scales.transpose(1, 2), format)
+
+
+class NewTokens:
+    """Owns a kvcrush_new_tokens_t: how many new tokens every sequence has and, with ``mask`` (int32 [total, words], bit j of
+    token i's row: i attends to token j of its sequence), who sees whom."""
+
+    def __init__(self, counts: Sequence[int], mask=None, device="cuda:0"):
+        import torch
+        self.counts = tuple(int(x) for x in counts)
+        self.cu_host = np.zeros(len(self.counts) + 1, dtype=np.int32)
+        self.cu_host[1:] = np.cumsum(np.asarray(self.counts, dtype=np.int64))
+        self.cu_dev = torch.from_numpy(self.cu_host).to(device)
+        self.total = int(self.cu_host[-1])
+        self.mask = mask
+        if mask is not None:
+            assert mask.dtype == torch.int32 and mask.dim() == 2 and mask.shape[0] == self.total and mask.is_contiguous()
+        self.struct = NewTokensStruct(self.total, max(self.counts, default=0), 0 if mask is None else int(mask.shape[1]), 0,
+                                      self.cu_host.ctypes.data, int(self.cu_dev.data_ptr()), _ptr(mask))
+        self.ref = ctypes.byref(self.struct)
+
+
+def _cache_refs(t):
+    """Descriptors of a tensor or a QuantTensor: values or codes, and scales or nothing."""
+    if isinstance(t, QuantTensor):
+        return ctypes.byref(t.struct), ctypes.byref(t.scales_struct)
+    return _tensor_ref(t), None
+
+
+def _tensor_ref(t):
+    return None if t is None else ctypes.byref(tensor_struct(t))
 
 
 def kvcrush_workspace_size(problem: Problem, stage: int) -> int:
@@ -282,6 +361,56 @@ def kvcrush_compact_pages(problem: Problem, k, v, page_size: int, cu_kept, page_
                                        int(page_size), _ptr(cu_kept), _ptr(page_idx), int(total_kept_pages),
                                        ctypes.byref(kos), ctypes.byref(vos) if vos is not None else None,
                                        _ptr(status), _stream() if stream is None else stream), "kvcrush_compact_pages")
+
+
+def kvcrush_quantize(problem: Problem, k, v, k_q: QuantTensor, v_q: Optional[QuantTensor], *, cu_kept=None, idx=None,
+                     total_kept: int = 0, in_begin=None, out_begin=None, status=None, stream: Optional[int] = None) -> None:
+    """Quantises rows of k and v [layers, tokens, heads, D] into k_q and v_q: kept rows (cu_kept, idx), or all of them."""
+    kc, ks = _cache_refs(k_q)
+    vc, vs = (None, None) if v_q is None else _cache_refs(v_q)
+    _check(lib().kvcrush_quantize(problem.ref, _tensor_ref(k), _tensor_ref(v), _ptr(cu_kept), _ptr(idx), int(total_kept),
+                                  _ptr(in_begin), _ptr(out_begin), kc, ks, vc, vs, _ptr(status),
+                                  _stream() if stream is None else stream), "kvcrush_quantize")
+
+
+def kvcrush_dequantize(problem: Problem, k_q: QuantTensor, v_q: Optional[QuantTensor], k, v, *, cu_kept=None, idx=None,
+                       total_kept: int = 0, in_begin=None, out_begin=None, status=None, stream: Optional[int] = None) -> None:
+    """Reads rows of a quantised cache back into k and v."""
+    kc, ks = _cache_refs(k_q)
+    vc, vs = (None, None) if v_q is None else _cache_refs(v_q)
+    _check(lib().kvcrush_dequantize(problem.ref, kc, ks, vc, vs, _ptr(cu_kept), _ptr(idx), int(total_kept), _ptr(in_begin),
+                                    _ptr(out_begin), _tensor_ref(k), _tensor_ref(v), _ptr(status),
+                                    _stream() if stream is None else stream), "kvcrush_dequantize")
+
+
+def kvcrush_attend(problem: Problem, new: NewTokens, q, k, v, out, *, k_new=None, v_new=None, lse=None, row_begin=None,
+                   row_count=None, status=None, stream: Optional[int] = None) -> None:
+    """Attention of new tokens q [layers, new.total, Hq, D] over a cache (tensors or QuantTensors) into out."""
+    kc, ks = _cache_refs(k)
+    vc, vs = _cache_refs(v)
+    _check(lib().kvcrush_attend(problem.ref, new.ref, _tensor_ref(q), kc, ks, vc, vs, _tensor_ref(k_new), _tensor_ref(v_new),
+                                _ptr(row_begin), _ptr(row_count), _tensor_ref(out), _ptr(lse), _ptr(status),
+                                _stream() if stream is None else stream), "kvcrush_attend")
+
+
+def kvcrush_page_bounds(problem: Problem, k, page_size: int, lo, hi, *, recent_pages: int = 0, row_begin=None, row_count=None,
+                        status=None, stream: Optional[int] = None) -> None:
+    """Least and largest key channels of every page (or of the last ones) into lo and hi [layers, n_seqs * max_pages, Hkv, D]."""
+    _check(lib().kvcrush_page_bounds(problem.ref, _tensor_ref(k), int(page_size), int(recent_pages), _ptr(row_begin),
+                                     _ptr(row_count), _tensor_ref(lo), _tensor_ref(hi), _ptr(status),
+                                     _stream() if stream is None else stream), "kvcrush_page_bounds")
+
+
+def kvcrush_attend_pages(problem: Problem, new: NewTokens, q, k, v, page_size: int, lo, hi, budget: int, out, *,
+                         keep_initial: int = 0, keep_recent: int = 0, page_idx=None, n_pages=None, lse=None, row_begin=None,
+                         row_count=None, status=None, stream: Optional[int] = None) -> None:
+    """Attention of new tokens over the `budget` pages whose bounds promise the largest logits."""
+    kc, ks = _cache_refs(k)
+    vc, vs = _cache_refs(v)
+    _check(lib().kvcrush_attend_pages(problem.ref, new.ref, _tensor_ref(q), kc, ks, vc, vs, int(page_size), _tensor_ref(lo),
+                                      _tensor_ref(hi), int(budget), int(keep_initial), int(keep_recent), _ptr(row_begin),
+                                      _ptr(row_count), _ptr(page_idx), _ptr(n_pages), _tensor_ref(out), _ptr(lse), _ptr(status),
+                                      _stream() if stream is None else stream), "kvcrush_attend_pages")
 
 
 class CompressionPass:

@@ -57,6 +57,7 @@ size_t signature_ws(const Shape& s) { return round_up((size_t)s.n_layers * s.n_s
 
 namespace kvc {
 int shape_from_problem(const kvcrush_problem_t* problem, Shape* out) { return make_shape(problem, out); }
+int view_from_tensor(const kvcrush_tensor_t* t, int head_dim, TensorView* v) { return make_view(t, head_dim, v); }
 }  // namespace kvc
 
 extern "C" {

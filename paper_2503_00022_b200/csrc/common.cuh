@@ -215,8 +215,73 @@ int launch_compact(const Shape& s, const TensorView& K, const TensorView* V, con
                    const int32_t* idx, long long total_kept, const TensorView& K_out, const TensorView* V_out,
                    cudaStream_t stream);
 
+// ---- quantised caches and the attention over them -----------------------------------------------------
+// A cache: token-major values or codes, and a row's float32 scale (INT4: scale and zero) where they are codes.
+struct CacheView {
+  const void* ptr;
+  int dtype;
+  long long sl, st, sh;        // strides in channels: layer, token, head
+  float* scales;               // NULL: values
+  long long scl, sct, sch;     // strides in floats
+};
+
+// Which rows a call moves (kvcrush_quantize): row i of the list.
+struct RowList {
+  const int32_t* cu_kept;      // NULL: all tokens
+  const int32_t* idx;          // NULL: consecutive rows
+  long long total;
+  const int32_t* in_begin;
+  const int32_t* out_begin;
+};
+// V.ptr may be NULL (K only).  One side is quantised, the other holds values.
+int launch_convert_rows(const Shape& s, const CacheView& K_in, const CacheView& V_in, const RowList& rows, const CacheView& K_out,
+                        const CacheView& V_out, cudaStream_t stream);
+
+struct NewTokens {
+  int total, most, mask_words;
+  const int32_t* cu;           // device, [n_seqs + 1]
+  const uint32_t* mask;
+};
+struct PageChoice {
+  int page_size, budget, keep_initial, keep_recent, max_pages;
+  TensorView lo, hi;
+  int32_t* page_idx;
+  int32_t* n_pages;
+};
+struct AttendArgs {
+  Shape s;
+  NewTokens fresh;
+  TensorView Q, K_new, V_new, O;   // K_new.ptr NULL: the new tokens are the last rows of the cache
+  CacheView K, V;
+  const int32_t* row_begin;
+  const int32_t* row_count;
+  float* lse;
+  float scale_log2;
+  int row_blocks;                  // blocks of query rows of a unit of work
+  PageChoice pages;                  // page_size 0: every row is read
+};
+int launch_attend(AttendArgs a, cudaStream_t stream);
+int launch_attend_simt(AttendArgs a, cudaStream_t stream);
+
+int launch_page_bounds(const Shape& s, const TensorView& K, int page_size, int recent_pages, const int32_t* row_begin,
+                       const int32_t* row_count, const TensorView& lo, const TensorView& hi, cudaStream_t stream);
+
+// Where the rows of a sequence start in its layer and how many there are; inside the layer whatever the arrays hold.
+__device__ __forceinline__ void rows_of(const Shape& s, const int32_t* __restrict__ row_begin, const int32_t* __restrict__ row_count,
+                                        int layer, int seq, int& begin, int& count) {
+  if (row_begin) {
+    const int seg = layer * s.n_seqs + seq;
+    begin = min(max(__ldg(row_begin + seg), 0), s.T);
+    count = min(max(__ldg(row_count + seg), 0), min(s.max_seqlen, s.T - begin));
+  } else {
+    begin = __ldg(s.cu_seqlens + seq);
+    count = __ldg(s.cu_seqlens + seq + 1) - begin;
+  }
+}
+
 // Validates a problem description and fills the device-side view (defined in api.cu).
 int shape_from_problem(const kvcrush_problem_t* problem, Shape* out);
+int view_from_tensor(const kvcrush_tensor_t* t, int head_dim, TensorView* v);
 
 inline int check_launch() { return cudaGetLastError() == cudaSuccess ? KVCRUSH_OK : KVCRUSH_ERR_CUDA; }
 
