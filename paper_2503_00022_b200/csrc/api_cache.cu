@@ -116,7 +116,15 @@ int make_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* ne
 }
 
 int dispatch_attend(const AttendArgs& a, void* stream) {
-  return launch_attend_simt(a, static_cast<cudaStream_t>(stream));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (a.Q.dtype == KVCRUSH_FP32) return launch_attend_simt(a, st);
+  switch (a.K.dtype) {
+    case KVCRUSH_BF16: return launch_attend_bf16(a, st);
+    case KVCRUSH_FP16: return launch_attend_fp16(a, st);
+    case KVCRUSH_INT8: return launch_attend_int8(a, st);
+    case KVCRUSH_E4M3: return launch_attend_e4m3(a, st);
+    default: return launch_attend_int4(a, st);
+  }
 }
 
 int pages_of(const Shape& s, int page_size) { return (int)(((long long)s.max_seqlen + page_size - 1) / page_size); }

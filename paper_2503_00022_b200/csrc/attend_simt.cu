@@ -299,12 +299,6 @@ int launch_formats(AttendArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-int launch_attend_simt(AttendArgs a, cudaStream_t stream) {
-  switch (a.Q.dtype) {
-    case KVCRUSH_BF16: return launch_formats<KVCRUSH_BF16>(a, stream);
-    case KVCRUSH_FP16: return launch_formats<KVCRUSH_FP16>(a, stream);
-    default: return launch_formats<KVCRUSH_FP32>(a, stream);
-  }
-}
+int launch_attend_simt(AttendArgs a, cudaStream_t stream) { return launch_formats<KVCRUSH_FP32>(a, stream); }
 
 }  // namespace kvc

@@ -260,8 +260,14 @@ struct AttendArgs {
   int row_blocks;                  // blocks of query rows of a unit of work
   PageChoice pages;                  // page_size 0: every row is read
 };
-int launch_attend(AttendArgs a, cudaStream_t stream);
+// float32 queries, caches of any type
 int launch_attend_simt(AttendArgs a, cudaStream_t stream);
+// 16-bit queries, by the type of the cache
+int launch_attend_bf16(AttendArgs a, cudaStream_t stream);
+int launch_attend_fp16(AttendArgs a, cudaStream_t stream);
+int launch_attend_int8(AttendArgs a, cudaStream_t stream);
+int launch_attend_e4m3(AttendArgs a, cudaStream_t stream);
+int launch_attend_int4(AttendArgs a, cudaStream_t stream);
 
 int launch_page_bounds(const Shape& s, const TensorView& K, int page_size, int recent_pages, const int32_t* row_begin,
                        const int32_t* row_count, const TensorView& lo, const TensorView& hi, cudaStream_t stream);
