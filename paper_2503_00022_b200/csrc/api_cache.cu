@@ -11,6 +11,7 @@ using namespace kvc;
 constexpr int kMaxHeadDim = 256;
 constexpr int kMaxNew = 1024;
 constexpr int kMaxPageSize = 1024;
+constexpr long long kMaxStep = 1LL << 31;            // bytes from one token to the next, in the attention kernels
 
 // Values (scales NULL) or codes with their scales.  `empty`: no row of it is read, so that it may have no memory.
 int make_cache(const kvcrush_tensor_t* t, const kvcrush_scales_t* scales, int head_dim, bool empty, CacheView* c) {
@@ -107,6 +108,8 @@ int make_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* ne
   if ((rc = make_cache(K, K_scales, s.D, s.T == 0, &a->K)) != KVCRUSH_OK) return rc;
   if ((rc = make_cache(V, V_scales, s.D, s.T == 0, &a->V)) != KVCRUSH_OK) return rc;
   if (a->O.dtype != a->Q.dtype || a->K.dtype != a->V.dtype || (!K_scales && a->K.dtype != a->Q.dtype)) return KVCRUSH_ERR_INVALID_ARG;
+  const int eb = elt_bytes(a->Q.dtype);
+  if (a->K.st * eb >= kMaxStep || a->V.st * eb >= kMaxStep || a->K.sct * 4 >= kMaxStep || a->V.sct * 4 >= kMaxStep) return KVCRUSH_ERR_UNSUPPORTED;
   a->row_begin = row_begin_dev;
   a->row_count = row_count_dev;
   a->lse = lse_out_dev;
@@ -165,6 +168,7 @@ int kvcrush_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t*
   if (K_new) {
     if ((rc = view_from_tensor(K_new, a.s.D, &a.K_new)) != KVCRUSH_OK) return rc;
     if ((rc = view_from_tensor(V_new, a.s.D, &a.V_new)) != KVCRUSH_OK) return rc;
+    if (a.K_new.st * elt_bytes(a.Q.dtype) >= kMaxStep || a.V_new.st * elt_bytes(a.Q.dtype) >= kMaxStep) return KVCRUSH_ERR_UNSUPPORTED;
     if (a.K_new.dtype != a.Q.dtype || a.V_new.dtype != a.Q.dtype) return KVCRUSH_ERR_INVALID_ARG;
   }
   return dispatch_attend(a, stream);

@@ -22,6 +22,11 @@ constexpr int kMaxCluster = 16;
 constexpr unsigned kAll = 0xFFFFFFFFu;
 
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xFF800000u); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // What exponentials are relative to; without a finite maximum all logits are -inf, which adds 0, or NaN, which stays.
 __device__ __forceinline__ float reference(float maximum) { return maximum == neg_inf() ? 0.f : maximum; }
 

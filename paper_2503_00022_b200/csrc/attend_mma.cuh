@@ -21,7 +21,6 @@ namespace att {
 
 using namespace fmt;
 
-constexpr int kWarps = 4;
 constexpr int kMaxDevices = 64;
 
 // ---- registers of a tile -----------------------------------------------------------------------------------
@@ -100,32 +99,37 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char
 
 // Where a tile's rows are: row numbers of its two halves of eight keys, and how many of each exist.
 struct Halves {
-  long long row[2];
+  int row[2];
   int n[2];
 };
 struct Source {
   const unsigned char *k, *v;                // of the layer and head
-  long long k_st, v_st;                      // bytes
+  uint32_t k_st, v_st;                       // bytes, below 2^31
   const float *ks, *vs;
-  long long k_sct, v_sct;
+  uint32_t k_sct, v_sct;                     // floats
 };
+template <class T> __device__ __forceinline__ const T* at_row(const T* base, int row, uint32_t stride) {
+  return base + (unsigned long long)(uint32_t)row * stride;
+}
 
 template <int F, int DP>
 struct KeyTile {
   using L = Layout<F, DP>;
   uint32_t a[2][L::kPieces][L::kWords];      // keys g and g + 8
   float2 sc[2];                              // scale (and zero)
+  // kFull: all 16 keys exist
+  template <bool kFull>
   __device__ __forceinline__ void load(const Source& s, const Halves& h, int D, int lane) {
     const int g = lane >> 2, c = lane & 3;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const bool there = g < h.n[j];
-      const unsigned char* p = s.k + (h.row[j] + g) * s.k_st;
+      const bool there = kFull || g < h.n[j];
+      const unsigned char* p = at_row(s.k, h.row[j] + g, s.k_st);
 #pragma unroll
       for (int i = 0; i < L::kPieces; ++i) load_words(a[j][i], p + bytes_of<F>(L::k_channel(i, c)), there && L::k_channel(i, c) < D);
       if constexpr (kQuantized<F>) {
         sc[j] = make_float2(0.f, 0.f);
-        const float* sp = s.ks + (h.row[j] + g) * s.k_sct;
+        const float* sp = at_row(s.ks, h.row[j] + g, s.k_sct);
         if (there) { if (F == KVCRUSH_INT4) sc[j] = __ldg(reinterpret_cast<const float2*>(sp)); else sc[j].x = __ldg(sp); }
       }
     }
@@ -149,12 +153,13 @@ struct ValueTile {
   }
   uint32_t a[4][L::kVPieces][L::kVWords];    // keys 2c, 2c + 1, 2c + 8, 2c + 9
   float2 sc[2];                              // keys g and g + 8
+  template <bool kFull>
   __device__ __forceinline__ void load(const Source& s, const Halves& h, int D, int lane) {
     const int g = lane >> 2, c = lane & 3;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool there = 2 * c + (j & 1) < h.n[j >> 1];
-      const unsigned char* p = s.v + (h.row[j >> 1] + 2 * c + (j & 1)) * s.v_st;
+      const bool there = kFull || 2 * c + (j & 1) < h.n[j >> 1];
+      const unsigned char* p = at_row(s.v, h.row[j >> 1] + 2 * c + (j & 1), s.v_st);
 #pragma unroll
       for (int i = 0; i < L::kVPieces; ++i) load_words(a[j][i], p + bytes_of<F>(channel(i, g)), there && channel(i, g) < D);
     }
@@ -162,8 +167,8 @@ struct ValueTile {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         sc[j] = make_float2(0.f, 0.f);
-        const float* sp = s.vs + (h.row[j] + g) * s.v_sct;
-        if (g < h.n[j]) { if (F == KVCRUSH_INT4) sc[j] = __ldg(reinterpret_cast<const float2*>(sp)); else sc[j].x = __ldg(sp); }
+        const float* sp = at_row(s.vs, h.row[j] + g, s.v_sct);
+        if (kFull || g < h.n[j]) { if (F == KVCRUSH_INT4) sc[j] = __ldg(reinterpret_cast<const float2*>(sp)); else sc[j].x = __ldg(sp); }
       }
     }
   }
@@ -268,8 +273,10 @@ __device__ __forceinline__ void logits(const KeyTile<F, DP>& K, const Queries& q
 }
 
 // Adds a tile to the running state.  x: logits (log2 domain), -inf where a key is not seen (then `hidden`, bit 4 n + i, says
-// so); F, A: the tile's type and the type it is multiplied in; kScaled: the state's output has a maximum of its own.
-template <int F, int FO, int A, int DP, int NB, bool kScaled>
+// so); F, A: the tile's type and the type it is multiplied in; kScaled: the state's output has a maximum of its own;
+// kFull: every key exists and is seen by all rows.  Maxima start at the lowest finite number, so that a logit of -inf
+// has weight 0 whatever came before.
+template <int F, int FO, int A, int DP, int NB, bool kScaled, bool kFull>
 __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const Source& src, const Halves& h, int D, float (&x)[NB][4], uint32_t hidden,
                                          bool masked, Running<NB, DP, kScaled>& run, int lane) {
   using L = Layout<F, DP>;
@@ -282,39 +289,49 @@ __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const So
       if (F == KVCRUSH_INT4) vz[j] = fmaf(8.f, V.sc[j].x, V.sc[j].y);
     }
   }
+  float d[NB][4], d2[NB][4];
+  auto differences = [&] {
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        d[n][i] = x[n][i] - run.m[n][i & 1];
+        if (kScaled) d2[n][i] = (x[n][i] + lv[i >> 1]) - run.m2[n][i & 1];
+      }
+  };
+  differences();
   // The maximum of a row seldom moves: the reduction over the tile's keys is done where any lane has a larger logit.
-  bool grow = false;
+  float most = 0.f;
 #pragma unroll
-  for (int n = 0; n < NB; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      grow |= x[n][i] > run.m[n][i & 1];
-      if (kScaled) grow |= x[n][i] + lv[i >> 1] > run.m2[n][i & 1];
-    }
-  if (__any_sync(kAll, grow)) {
+  for (int n = 0; n < NB; ++n) {
+    most = fmaxf(fmaxf(most, fmaxf(d[n][0], d[n][1])), fmaxf(d[n][2], d[n][3]));
+    if (kScaled) most = fmaxf(fmaxf(most, fmaxf(d2[n][0], d2[n][1])), fmaxf(d2[n][2], d2[n][3]));
+  }
+  if (__any_sync(kAll, most > 0.f)) {
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         float big = fmaxf(x[n][i], x[n][i + 2]), big2 = kScaled ? fmaxf(x[n][i] + lv[0], x[n][i + 2] + lv[1]) : 0.f;
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-          big = fmaxf(big, __shfl_xor_sync(kAll, big, d));
-          if (kScaled) big2 = fmaxf(big2, __shfl_xor_sync(kAll, big2, d));
+        for (int k = 4; k < 32; k <<= 1) {
+          big = fmaxf(big, __shfl_xor_sync(kAll, big, k));
+          if (kScaled) big2 = fmaxf(big2, __shfl_xor_sync(kAll, big2, k));
         }
-        const float m = fmaxf(run.m[n][i], big), f = exp2f(run.m[n][i] - reference(m));
+        const float m = fmaxf(run.m[n][i], big), f = ex2(run.m[n][i] - m);
         run.m[n][i] = m;
         run.l[n][i] *= f;
         if (kScaled) run.b[n][i] *= f;
         float f2 = f;
         if constexpr (kScaled) {
           const float m2 = fmaxf(run.m2[n][i], big2);
-          f2 = exp2f(run.m2[n][i] - reference(m2));
+          f2 = ex2(run.m2[n][i] - m2);
           run.m2[n][i] = m2;
         }
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) { run.o[n][t][i] *= f2; run.o[n][t][i + 2] *= f2; }
       }
+    differences();
   }
   uint32_t b0[NB], b1[NB];
 #pragma unroll
@@ -322,20 +339,20 @@ __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const So
     float w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float p = exp2f(x[n][i] - reference(run.m[n][i & 1]));
+      const float p = ex2(d[n][i]);
+      const bool unseen = !kFull && (hidden >> (4 * n + i) & 1u);
       run.l[n][i & 1] += p;
       w[i] = p;
       if constexpr (kScaled) {
-        if (F == KVCRUSH_INT4) run.b[n][i & 1] = fmaf(p, (hidden >> (4 * n + i) & 1u) ? 0.f : vz[i >> 1], run.b[n][i & 1]);
-        w[i] = exp2f(x[n][i] + lv[i >> 1] - reference(run.m2[n][i & 1]));
-        if (kQuantized<F> && (hidden >> (4 * n + i) & 1u)) w[i] = 0.f;
+        if (F == KVCRUSH_INT4) run.b[n][i & 1] = fmaf(p, unseen ? 0.f : vz[i >> 1], run.b[n][i & 1]);
+        w[i] = kQuantized<F> && unseen ? 0.f : ex2(d2[n][i]);
       }
     }
     x[n][0] = w[0]; x[n][1] = w[1]; x[n][2] = w[2]; x[n][3] = w[3];
     b0[n] = transpose8x8(A == KVCRUSH_BF16 ? pack_bf16(w[0], w[1]) : pack_fp16(w[0], w[1]));
     b1[n] = transpose8x8(A == KVCRUSH_BF16 ? pack_bf16(w[2], w[3]) : pack_fp16(w[2], w[3]));
   }
-  if (masked) {
+  if (!kFull && masked) {
     // A weight of 0 takes a value that is not finite along: where there is one, every row adds up the keys that it sees.
     bool bad = false;
 #pragma unroll
@@ -349,7 +366,7 @@ __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const So
 #pragma unroll 1
       for (int key = 0; key < kTile; ++key) {
         if ((key & 7) >= h.n[key >> 3]) continue;
-        const unsigned char* row = src.v + (h.row[key >> 3] + (key & 7)) * src.v_st;
+        const unsigned char* row = at_row(src.v, h.row[key >> 3] + (key & 7), src.v_st);
         const uint32_t hid = __shfl_sync(kAll, hidden, (key & 7) * 4 + c);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
@@ -392,7 +409,7 @@ __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const So
 // ---- the kernel ---------------------------------------------------------------------------------------------------
 
 // Byte offsets in dynamic shared memory.
-template <int F, int FQ, int DP, int NB>
+template <int F, int FQ, int DP, int NB, int kWarps>
 struct Mem {
   static constexpr int kRows = 8 * NB;
   static constexpr int kQStride = DP * 2 + 16, kOStride = DP + 4;
@@ -405,14 +422,16 @@ struct Mem {
   static constexpr int kEnd = kO + kWarps * kRows * kOStride * 4;
 };
 
-template <int F, int FQ, int DP, int NB, bool kPages>
-__global__ void __launch_bounds__(kWarps * 32)
+template <int F, int FQ, int DP, int NB, int kWarps, int kBlocks, bool kPages>
+__global__ void __launch_bounds__(kWarps * 32, kBlocks)
 attend_kernel(AttendArgs a) {
-  using M = Mem<F, FQ, DP, NB>;
+  using M = Mem<F, FQ, DP, NB, kWarps>;
   using L = Layout<F, DP>;
   constexpr bool kScaled = kQuantized<F>;
   constexpr int A = kArith<F, FQ>, kRows = M::kRows;
-  constexpr bool kRegs = NB * DP <= 128;
+  // Keys of a tile that take few registers are loaded a tile ahead; otherwise other warps' loads fill the time.
+  constexpr bool kAhead = DP * Bits<F>::value <= 1024;
+  constexpr bool kRegs = NB * DP <= 128 && kAhead;             // queries in registers
   extern __shared__ __align__(16) unsigned char sh[];
   chain_wait();
   chain_trigger();
@@ -487,7 +506,7 @@ attend_kernel(AttendArgs a) {
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) { run.m[n][i] = run.m2[n][i] = neg_inf(); run.l[n][i] = run.b[n][i] = 0.f; }
+    for (int i = 0; i < 2; ++i) { run.m[n][i] = run.m2[n][i] = -FLT_MAX; run.l[n][i] = run.b[n][i] = 0.f; }
 #pragma unroll
     for (int t = 0; t < DP / 16; ++t)
 #pragma unroll
@@ -496,13 +515,21 @@ attend_kernel(AttendArgs a) {
 
   const Source src{static_cast<const unsigned char*>(a.K.ptr) + bytes_of<F>(w.layer * a.K.sl + w.hk * a.K.sh),
                    static_cast<const unsigned char*>(a.V.ptr) + bytes_of<F>(w.layer * a.V.sl + w.hk * a.V.sh),
-                   bytes_of<F>(a.K.st), bytes_of<F>(a.V.st), a.K.scales + w.layer * a.K.scl + w.hk * a.K.sch,
-                   a.V.scales + w.layer * a.V.scl + w.hk * a.V.sch, a.K.sct, a.V.sct};
+                   (uint32_t)bytes_of<F>(a.K.st), (uint32_t)bytes_of<F>(a.V.st), a.K.scales + w.layer * a.K.scl + w.hk * a.K.sch,
+                   a.V.scales + w.layer * a.V.scl + w.hk * a.V.sch, (uint32_t)a.K.sct, (uint32_t)a.V.sct};
   const int halves_per_page = kPages ? a.pages.page_size / 8 : 1;
   const int cached = kPages ? (n_chosen * halves_per_page + 1) / 2 : (w.seen + kTile - 1) / kTile;
   const int n_tiles = cached + (w.own + kTile - 1) / kTile;
   const int per = (n_tiles + n_blk - 1) / n_blk, lo = min(n_tiles, rank * per), hi = min(n_tiles, lo + per), hi_cached = min(hi, cached);
-  const int unmasked = w.own ? w.seen : w.limit(s.G, 0);              // rows of the cache that every query row sees
+  // tiles whose keys all exist and are seen by every query row; of the chosen pages only the last may be short
+  int full;
+  if (kPages) {
+    const int last = n_chosen ? pages.chosen[n_chosen - 1] : 0;
+    full = n_chosen ? ((n_chosen - 1) * a.pages.page_size + min(a.pages.page_size, w.seen - last * a.pages.page_size)) / kTile : 0;
+  } else {
+    full = (w.own ? w.seen : w.limit(s.G, 0)) / kTile;
+  }
+  const int hi_full = min(hi, full);
   auto halves = [&](int t) {
     Halves h;
 #pragma unroll
@@ -515,19 +542,11 @@ attend_kernel(AttendArgs a) {
         pos = there ? pages.chosen[page] * a.pages.page_size + (hn - page * halves_per_page) * 8 : 0;
       }
       h.n[j] = there ? min(8, max(0, w.seen - pos)) : 0;
-      h.row[j] = (long long)w.begin + pos;
+      h.row[j] = w.begin + pos;
     }
     return h;
   };
-  // a tile of the cache whose keys have arrived
-  auto step = [&](int t, const Halves& h, KeyTile<F, DP>& K, auto&& prefetch) {
-    ValueTile<F, DP> V;
-    V.load(src, h, s.D, lane);
-    prefetch();
-    float x[NB][4];
-    logits<F, A, DP, NB, kRegs>(K, q, qr, lane, x);
-    uint32_t hidden = 0;
-    const bool masked = !kPages && t * kTile + kTile > unmasked, ragged = h.n[0] + h.n[1] < kTile;
+  auto scale_logits = [&](const KeyTile<F, DP>& K, float (&x)[NB][4]) {
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -539,49 +558,77 @@ attend_kernel(AttendArgs a) {
           x[n][i] *= a.scale_log2;
         }
       }
-    if (masked || ragged) {
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = n * 8 + 2 * c + (i & 1);
-          if (g >= h.n[i >> 1] || (masked && t * kTile + g + (i >> 1) * 8 >= w.limit(s.G, min(r, w.rows - 1)))) {
-            x[n][i] = neg_inf();
-            hidden |= 1u << (4 * n + i);
-          }
-        }
-    }
-    add_tile<F, F, A, DP, NB, kScaled>(V, src, h, s.D, x, hidden, masked, run, lane);
   };
   {
-    // while a tile is multiplied the next one's keys are in flight
-    KeyTile<F, DP> k0, k1;
+    auto step = [&](const Halves& h, const KeyTile<F, DP>& K, auto&& prefetch) {
+      ValueTile<F, DP> V;
+      V.template load<true>(src, h, s.D, lane);
+      prefetch();
+      float x[NB][4];
+      logits<F, A, DP, NB, kRegs>(K, q, qr, lane, x);
+      scale_logits(K, x);
+      add_tile<F, F, A, DP, NB, kScaled, true>(V, src, h, s.D, x, 0u, false, run, lane);
+    };
     int t = lo + warp;
-    Halves h0, h1;
-    if (t < hi_cached) { h0 = halves(t); k0.load(src, h0, s.D, lane); }
-    for (; t < hi_cached; t += 2 * kWarps) {
-      step(t, h0, k0, [&] { if (t + kWarps < hi_cached) { h1 = halves(t + kWarps); k1.load(src, h1, s.D, lane); } });
-      if (t + kWarps >= hi_cached) break;
-      step(t + kWarps, h1, k1, [&] { if (t + 2 * kWarps < hi_cached) { h0 = halves(t + 2 * kWarps); k0.load(src, h0, s.D, lane); } });
+    if constexpr (kAhead) {
+      // while a tile is multiplied the next one's keys are in flight
+      KeyTile<F, DP> k0, k1;
+      Halves h0, h1;
+      if (t < hi_full) { h0 = halves(t); k0.template load<true>(src, h0, s.D, lane); }
+      for (; t < hi_full; t += 2 * kWarps) {
+        step(h0, k0, [&] { if (t + kWarps < hi_full) { h1 = halves(t + kWarps); k1.template load<true>(src, h1, s.D, lane); } });
+        if (t + kWarps >= hi_full) break;
+        step(h1, k1, [&] { if (t + 2 * kWarps < hi_full) { h0 = halves(t + 2 * kWarps); k0.template load<true>(src, h0, s.D, lane); } });
+      }
+    } else {
+      for (; t < hi_full; t += kWarps) {
+        const Halves h = halves(t);
+        KeyTile<F, DP> K;
+        K.template load<true>(src, h, s.D, lane);
+        step(h, K, [] {});
+      }
     }
+  }
+  // short tiles, and those that some rows see only a part of
+  for (int t = max(lo, full) + warp; t < hi_cached; t += kWarps) {
+    const Halves h = halves(t);
+    KeyTile<F, DP> K;
+    ValueTile<F, DP> V;
+    K.template load<false>(src, h, s.D, lane);
+    V.template load<false>(src, h, s.D, lane);
+    float x[NB][4];
+    logits<F, A, DP, NB, kRegs>(K, q, qr, lane, x);
+    scale_logits(K, x);
+    uint32_t hidden = 0;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = n * 8 + 2 * c + (i & 1);
+        if (g >= h.n[i >> 1] || (!kPages && t * kTile + g + (i >> 1) * 8 >= w.limit(s.G, min(r, w.rows - 1)))) {
+          x[n][i] = neg_inf();
+          hidden |= 1u << (4 * n + i);
+        }
+      }
+    add_tile<F, F, A, DP, NB, kScaled, false>(V, src, h, s.D, x, hidden, true, run, lane);
   }
   // keys among the new tokens
   if (!kPages && w.own && hi > cached) {
     const Source fresh{static_cast<const unsigned char*>(a.K_new.ptr) + bytes_of<FQ>(w.layer * a.K_new.sl + w.hk * a.K_new.sh),
                        static_cast<const unsigned char*>(a.V_new.ptr) + bytes_of<FQ>(w.layer * a.V_new.sl + w.hk * a.V_new.sh),
-                       bytes_of<FQ>(a.K_new.st), bytes_of<FQ>(a.V_new.st), nullptr, nullptr, 0, 0};
+                       (uint32_t)bytes_of<FQ>(a.K_new.st), (uint32_t)bytes_of<FQ>(a.V_new.st), nullptr, nullptr, 0, 0};
     for (int t = max(lo, cached) + warp; t < hi; t += kWarps) {
       const int first = (t - cached) * kTile;
       Halves h;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        h.row[j] = (long long)w.first + first + j * 8;
+        h.row[j] = w.first + first + j * 8;
         h.n[j] = min(8, max(0, w.own - first - j * 8));
       }
       KeyTile<FQ, DP> K;
       ValueTile<FQ, DP, F> V;
-      K.load(fresh, h, s.D, lane);
-      V.load(fresh, h, s.D, lane);
+      K.template load<false>(fresh, h, s.D, lane);
+      V.template load<false>(fresh, h, s.D, lane);
       float x[NB][4];
       const uint32_t none[1] = {0u};
       logits<FQ, FQ, DP, NB, false>(K, q_new, none, lane, x);
@@ -597,7 +644,7 @@ attend_kernel(AttendArgs a) {
             hidden |= 1u << (4 * n + i);
           }
         }
-      add_tile<FQ, F, FQ, DP, NB, kScaled>(V, fresh, h, s.D, x, hidden, true, run, lane);
+      add_tile<FQ, F, FQ, DP, NB, kScaled, false>(V, fresh, h, s.D, x, hidden, true, run, lane);
     }
   }
 
@@ -624,16 +671,16 @@ attend_kernel(AttendArgs a) {
     }
   __syncthreads();
   if (tid < kRows) {
-    float m = neg_inf(), l = 0.f, m2 = neg_inf(), b = 0.f;
+    float m = -FLT_MAX, l = 0.f, m2 = -FLT_MAX, b = 0.f;
     for (int k = 0; k < kWarps; ++k) { m = fmaxf(m, warp_part[k * kRows + tid].m); m2 = fmaxf(m2, warp_part[k * kRows + tid].m2); }
     for (int k = 0; k < kWarps; ++k) {
       Part& p = warp_part[k * kRows + tid];
-      const float f = p.l == 0.f ? 0.f : exp2f(p.m - reference(m));
+      const float f = ex2(p.m - m);
       l = fmaf(p.l, f, l);
       b = fmaf(p.b, f, b);
-      p.b = exp2f(p.m2 - reference(m2));                              // factor of the warp's output
+      p.b = ex2(p.m2 - m2);                              // factor of the warp's output
     }
-    part[tid] = Part{m, l, reference(m2), b};
+    part[tid] = Part{m, l, m2, b};
   }
   __syncthreads();
   for (int e = tid; e < w.rows * (DP / 4); e += kWarps * 32) {
@@ -655,7 +702,7 @@ attend_kernel(AttendArgs a) {
 // Largest cluster of this kernel that the device runs (write-once cache per device): 16 blocks are more than every device
 // grants.
 template <class Kernel>
-int largest_cluster(Kernel kern, size_t dyn, std::atomic<int>* known) {
+int largest_cluster(Kernel kern, int threads, size_t dyn, std::atomic<int>* known) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return 8; }
   int n = known[dev].load(std::memory_order_relaxed);
@@ -663,7 +710,7 @@ int largest_cluster(Kernel kern, size_t dyn, std::atomic<int>* known) {
   n = 8;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kMaxCluster);
-  cfg.blockDim = dim3(kWarps * 32);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = dyn;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
@@ -682,8 +729,10 @@ int largest_cluster(Kernel kern, size_t dyn, std::atomic<int>* known) {
 
 template <int F, int FQ, int DP, int NB, bool kPages>
 int launch_one(AttendArgs& a, cudaStream_t stream) {
-  auto kern = attend_kernel<F, FQ, DP, NB, kPages>;
-  using M = Mem<F, FQ, DP, NB>;
+  // Two blocks an SM at least: a chip has room for 14 clusters of 16 then, with one only for 7.
+  constexpr int kWarps = NB * DP <= 128 ? 8 : 4, kBlocks = NB * DP == 256 ? 3 : 2;
+  auto kern = attend_kernel<F, FQ, DP, NB, kWarps, kBlocks, kPages>;
+  using M = Mem<F, FQ, DP, NB, kWarps>;
   const Shape& s = a.s;
   const long long rows = (long long)(kPages ? 1 : a.fresh.most) * s.G;
   a.row_blocks = (int)((rows + M::kRows - 1) / M::kRows);
@@ -695,7 +744,7 @@ int launch_one(AttendArgs& a, cudaStream_t stream) {
   constexpr int bound = most + (kPages ? kMaxPagesPerSeq * 12 + 256 * 16 + 2048 : 0);
   if (allow_dynamic_smem(kern, bound) != KVCRUSH_OK) return KVCRUSH_ERR_CUDA;
   static std::atomic<int> known[kMaxDevices];
-  const int n_blk = cluster_size(units, (int)((keys + kTile - 1) / kTile), kWarps, largest_cluster(kern, bound, known), 2 * sm_count());
+  const int n_blk = cluster_size(units, (int)((keys + kTile - 1) / kTile), kWarps, largest_cluster(kern, kWarps * 32, bound, known), 4 * sm_count());
   if (units * n_blk > 0x7FFFFFFFLL) return KVCRUSH_ERR_UNSUPPORTED;
   return launch_chained(kern, dim3((unsigned)(units * n_blk)), dim3(kWarps * 32), dyn, stream, n_blk, a);
 }

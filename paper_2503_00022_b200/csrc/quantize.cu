@@ -2,14 +2,15 @@
 // representation of that cache is independent of which tokens are kept).
 //
 // Bound by HBM bandwidth: every row is read once, gathered by the kept list, and written once.  A row (one token, one KV
-// head) belongs to 8, 16 or 32 lanes of eight channels each; its largest magnitude (INT4: least and largest value) is
-// found by shuffles while the row stays in registers.
+// head) belongs to 4, 8 or 16 lanes with one to three pieces of eight channels each; its largest magnitude (INT4: least and
+// largest value) is found by shuffles while the row stays in registers.
 //
 // Codes are quotients rounded to the nearest code.  Rows of 16-bit values have few significant bits, so that quotients often
 // lie on the border between two codes exactly, and a product with a rounded reciprocal would fall on either side.  The
 // quotient is therefore corrected by its remainder (one Newton step, Markstein 1990: q' = q + (a - q b) / b with both steps as
 // fused multiply-adds), which gives the nearest float32 to a / b and so exact ties.
 #include "cache_format.cuh"
+#include "tc_ptx.cuh"
 
 namespace kvc {
 
@@ -18,174 +19,245 @@ namespace {
 using namespace fmt;
 
 constexpr int kWarps = 8;
-constexpr int kSteps = 4;                    // rows of a lane group in flight
 
 struct ConvertArgs {
   CacheView in[2], out[2];
   RowList rows;
-  int items_per_row;                         // of one tensor
+  int chunks;                                // groups of heads of a row that a warp takes at a time
+  int rows_per_warp;                         // 1 .. 32 rows of the list
 };
 
 template <int F> __device__ constexpr float top_code() { return F == KVCRUSH_INT8 ? 127.f : F == KVCRUSH_E4M3 ? 448.f : 15.f; }
 
-// a / b, correctly rounded but for results near the ends of the range; inv: 1 / b rounded.
-__device__ __forceinline__ float quotient(float a, float b, float inv) {
-  const float q = a * inv;
-  return fmaf(fmaf(-q, b, a), inv, q);
+// Two quotients a / b to the nearest float32 but near the ends of the range; inv: 1 / b to an ulp.
+__device__ __forceinline__ tc::f32x2 quotient2(tc::f32x2 a, tc::f32x2 minus_b, tc::f32x2 inv) {
+  const tc::f32x2 q = tc::mul2(a, inv);
+  return tc::fma2(tc::fma2(q, minus_b, a), inv, q);
+}
+__device__ __forceinline__ float reciprocal(float b) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(b));
+  return fmaf(fmaf(-r, b, 1.f), r, r);
+}
+// the larger magnitude; NaN if either is NaN
+__device__ __forceinline__ float larger(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
 }
 
-// Codes of eight channels of a row whose kLanes lanes call this together; scale (and zero) come back in every lane.
-template <int F, int kLanes>
-__device__ __forceinline__ void quantize8(float (&x)[8], int lanes_used, Raw8<F>& codes, float& scale, float& zero) {
-  uint32_t big = 0;                          // order of magnitudes as integers: NaN behind infinity behind the rest
-  float lo = x[0], hi = x[0];
+// Codes of the pieces of a row whose kLanes lanes call this together; scale (and zero) come back in every lane.  there: which of
+// the lane's pieces exist.
+template <int F, int kLanes, int kVecs>
+__device__ __forceinline__ void quantize_row(const float (&x)[kVecs][8], const bool (&there)[kVecs], Raw8<F> (&codes)[kVecs], float& scale,
+                                             float& zero) {
+  float big = 0.f, lo = FLT_MAX, hi = -FLT_MAX;      // pieces that do not exist are zeros
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    big = max(big, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    if (F == KVCRUSH_INT4) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
+  for (int v = 0; v < kVecs; ++v) {
+    float l = x[v][0], h = x[v][0];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (F == KVCRUSH_INT4) { l = fminf(l, x[v][i]); h = larger(h, x[v][i]); }
+      else big = larger(big, fabsf(x[v][i]));
+    }
+    if (F == KVCRUSH_INT4 && there[v]) { lo = fminf(lo, l); hi = larger(hi, h); }
   }
-  const bool used = (threadIdx.x & (kLanes - 1)) < lanes_used;
-  if (!used) { big = 0; lo = FLT_MAX; hi = -FLT_MAX; }
 #pragma unroll
   for (int d = 1; d < kLanes; d <<= 1) {
-    big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, d));
     if (F == KVCRUSH_INT4) {
       lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, d));
-      hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, d));
+      hi = larger(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, d));
+    } else {
+      big = larger(big, __shfl_xor_sync(0xFFFFFFFFu, big, d));
     }
   }
-  zero = F == KVCRUSH_INT4 ? lo : 0.f;
-  const float span = F == KVCRUSH_INT4 ? hi - lo : __uint_as_float(big);
+  const float span = F == KVCRUSH_INT4 ? hi - lo : big;
   scale = span * (1.f / top_code<F>());
-  const bool bad = big >= 0x7F800000u || !(span <= FLT_MAX);
+  zero = F == KVCRUSH_INT4 ? lo : 0.f;
+  const bool bad = !(span <= FLT_MAX);               // a NaN or an infinity, or INT4's span overflows
+  if (scale < 0x1p-126f) scale = 0.f;
   if (bad) scale = zero = __uint_as_float(0x7FC00000u);
-  else if (scale < 0x1p-126f) scale = 0.f;
   // a power of two that keeps products and remainders away from both ends of the range
   const float shift = span > 0x1p64f ? 0x1p-64f : span < 0x1p-64f ? 0x1p64f : 1.f;
-  const float num = top_code<F>() * shift, den = span * shift;
-  const float inv = __frcp_rn(den);
-  const bool none = bad || scale == 0.f;
-  uint32_t c[8];
+  const uint32_t keep = bad || scale == 0.f ? 0u : ~0u;
+  const float den = span * shift;
+  const tc::f32x2 num = tc::splat2(top_code<F>() * shift), minus_den = tc::splat2(-den), inv = tc::splat2(reciprocal(den)), minus_lo = tc::splat2(-lo);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = quotient((F == KVCRUSH_INT4 ? x[i] - lo : x[i]) * num, den, inv);
-    if (F == KVCRUSH_E4M3) c[i] = __float_as_uint(none ? 0.f : y);
-    else c[i] = none ? 0u : __float_as_uint(y + 12582912.f);       // 1.5 * 2^23: the nearest integer in the low bits, ties to even
-  }
-  if constexpr (F == KVCRUSH_INT8) {
+  for (int v = 0; v < kVecs; ++v) {
+    uint32_t c[8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      codes.w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
-  } else if constexpr (F == KVCRUSH_E4M3) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(__uint_as_float(c[4 * i]), __uint_as_float(c[4 * i + 1])), __NV_SATFINITE, __NV_E4M3);
-      const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(__uint_as_float(c[4 * i + 2]), __uint_as_float(c[4 * i + 3])), __NV_SATFINITE, __NV_E4M3);
-      codes.w[i] = a | b << 16;
+    for (int i = 0; i < 8; i += 2) {
+      tc::f32x2 y = tc::pack2f(x[v][i], x[v][i + 1]);
+      if (F == KVCRUSH_INT4) y = tc::add2(y, minus_lo);
+      y = quotient2(tc::mul2(y, num), minus_den, inv);
+      if (F != KVCRUSH_E4M3) y = tc::add2(y, tc::splat2(12582912.f));   // 1.5 * 2^23 on top: the nearest integer in the low bits, ties to even
+      float y0, y1;
+      tc::unpack2(y, y0, y1);
+      c[i] = __float_as_uint(y0); c[i + 1] = __float_as_uint(y1);
     }
-  } else {
-    codes.w[0] = 0;
+    Raw8<F>& out = codes[v];
+    if constexpr (F == KVCRUSH_INT8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) codes.w[0] |= (c[i] & 15u) << (4 * i);
+      for (int i = 0; i < 2; ++i)
+        out.w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410) & keep;
+    } else if constexpr (F == KVCRUSH_E4M3) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(__uint_as_float(c[4 * i]), __uint_as_float(c[4 * i + 1])), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(__uint_as_float(c[4 * i + 2]), __uint_as_float(c[4 * i + 3])), __NV_SATFINITE, __NV_E4M3);
+        out.w[i] = (a | b << 16) & keep;
+      }
+    } else {
+      // nibbles of four channels pair up by a shift, bytes by a permutation
+      uint32_t p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = (c[2 * i] & 15u) | c[2 * i + 1] << 4;
+      out.w[0] = __byte_perm(__byte_perm(p[0], p[1], 0x0040), __byte_perm(p[2], p[3], 0x0040), 0x5410) & keep;
+    }
   }
 }
 
-// One warp: kSteps * 32 / kLanes heads of one token of one tensor.
-template <int FI, int FO, int kLanes>
-__global__ void __launch_bounds__(kWarps * 32)
+// A row has kLanes lanes of kVecs pieces.  One warp: kSteps * 32 / kLanes heads of one tensor, for a few consecutive rows of the list.  Where the rows come from and go
+// to is found for all of them at once, a lane a row, since it takes a chain of dependent loads.
+template <int FI, int FO, int kLanes, int kVecs, int kSteps>
+__global__ void __launch_bounds__(kWarps * 32, 3)
 convert_kernel(Shape s, ConvertArgs a, int n_tensors) {
   chain_wait();
   chain_trigger();
   constexpr int kRowsPerStep = 32 / kLanes;
   const int lane = threadIdx.x & 31;
   const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int per_row = a.items_per_row * n_tensors;
-  const long long row = item / per_row;
-  if (row >= a.rows.total) return;
-  const int part = (int)(item - row * per_row), ten = part / a.items_per_row, chunk = part - ten * a.items_per_row;
-  int layer, seq;
-  long long src, dst;
-  if (a.rows.cu_kept) {
-    const int n_seg = s.n_layers * s.n_seqs;
-    if (row >= __ldg(a.rows.cu_kept + n_seg)) return;               // `total` is an upper bound
-    const int seg = warp_segment_of_row(a.rows.cu_kept, n_seg, row, lane);
-    layer = seg / s.n_seqs;
-    seq = seg - layer * s.n_seqs;
-    const int first = __ldg(a.rows.cu_kept + seg);
-    src = a.rows.idx ? (long long)__ldg(a.rows.idx + row) : row - first;
-    dst = row - first;
-    src += a.rows.in_begin ? __ldg(a.rows.in_begin + seg) : __ldg(s.cu_seqlens + seq);
-    dst += a.rows.out_begin ? __ldg(a.rows.out_begin + seg) : first - __ldg(a.rows.cu_kept + layer * s.n_seqs);
-  } else {
-    layer = (int)(row / s.T);
-    const int tok = (int)(row - (long long)layer * s.T);
-    src = dst = tok;
-    if (a.rows.in_begin || a.rows.out_begin) {
-      seq = seq_of_token(s.cu_seqlens, s.n_seqs, tok);
-      const int seg = layer * s.n_seqs + seq, off = tok - __ldg(s.cu_seqlens + seq);
-      if (a.rows.in_begin) src = __ldg(a.rows.in_begin + seg) + (long long)off;
-      if (a.rows.out_begin) dst = __ldg(a.rows.out_begin + seg) + (long long)off;
+  const int per_group = a.chunks * n_tensors;
+  const long long row0 = (item <= 0x7FFFFFFF ? (long long)((unsigned)item / (unsigned)per_group) : item / per_group) * a.rows_per_warp;
+  long long end = a.rows.total;
+  const int n_seg = s.n_layers * s.n_seqs;
+  if (a.rows.cu_kept) end = min(end, (long long)__ldg(a.rows.cu_kept + n_seg));      // `total` is an upper bound
+  if (row0 >= end) return;
+  const int part = (int)(item % per_group), ten = part / a.chunks, chunk = part - ten * a.chunks;
+  const int n_rows = (int)min((long long)a.rows_per_warp, end - row0);
+  int layer = 0;
+  long long src = 0, dst = 0;
+  int seg = a.rows.cu_kept ? warp_segment_of_row(a.rows.cu_kept, n_seg, row0, lane) : 0;
+  if (lane < n_rows) {
+    const long long row = row0 + lane;
+    if (a.rows.cu_kept) {
+      while (seg + 1 < n_seg && (long long)__ldg(a.rows.cu_kept + seg + 1) <= row) ++seg;   // later rows may belong to a later segment
+      layer = seg / s.n_seqs;
+      const int seq = seg - layer * s.n_seqs, first = __ldg(a.rows.cu_kept + seg);
+      src = (a.rows.idx ? (long long)__ldg(a.rows.idx + row) : row - first) + (a.rows.in_begin ? __ldg(a.rows.in_begin + seg) : __ldg(s.cu_seqlens + seq));
+      dst = row - first + (a.rows.out_begin ? __ldg(a.rows.out_begin + seg) : first - __ldg(a.rows.cu_kept + layer * s.n_seqs));
+    } else {
+      layer = (int)(row / s.T);
+      const int tok = (int)(row - (long long)layer * s.T);
+      src = dst = tok;
+      if (a.rows.in_begin || a.rows.out_begin) {
+        const int seq = seq_of_token(s.cu_seqlens, s.n_seqs, tok), off = tok - __ldg(s.cu_seqlens + seq);
+        seg = layer * s.n_seqs + seq;
+        if (a.rows.in_begin) src = __ldg(a.rows.in_begin + seg) + (long long)off;
+        if (a.rows.out_begin) dst = __ldg(a.rows.out_begin + seg) + (long long)off;
+      }
     }
   }
   const CacheView in = a.in[ten], out = a.out[ten];
-  const int sub = lane & (kLanes - 1), lanes_used = s.D / 8, ch = sub * 8;
-  const unsigned char* ip = static_cast<const unsigned char*>(in.ptr) + bytes_of<FI>(layer * in.sl + src * in.st + ch);
-  unsigned char* op = static_cast<unsigned char*>(const_cast<void*>(out.ptr)) + bytes_of<FO>(layer * out.sl + dst * out.st + ch);
+  const int sub = lane & (kLanes - 1);
   const int h0 = chunk * kSteps * kRowsPerStep + lane / kLanes;
-  Raw8<FI> raw[kSteps];
-  float2 sc[kSteps];
+  // offsets of the lane's first row: in and out in channels, scales of the quantised side in floats
+  const long long ib = layer * in.sl + src * in.st, ob = layer * out.sl + dst * out.st;
+  const long long sb = kQuantized<FI> ? layer * in.scl + src * in.sct : layer * out.scl + dst * out.sct;
+  const unsigned char* ip = static_cast<const unsigned char*>(in.ptr) + bytes_of<FI>(sub * 8);
+  unsigned char* op = static_cast<unsigned char*>(const_cast<void*>(out.ptr)) + bytes_of<FO>(sub * 8);
+  constexpr int kPiece = kLanes * 8;                 // channels from a lane's piece to its next
+  bool exists[kVecs];
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u) {
-    const int h = h0 + u * kRowsPerStep;
+  for (int v = 0; v < kVecs; ++v) exists[v] = sub * 8 + v * kPiece < s.D;
+  Raw8<FI> next[kSteps][kVecs];
+  float2 next_sc[kSteps];
+  auto load = [&](int r) {
+    const long long ir = __shfl_sync(0xFFFFFFFFu, ib, r), sr = __shfl_sync(0xFFFFFFFFu, sb, r);
 #pragma unroll
-    for (int i = 0; i < Raw8<FI>::kWords; ++i) raw[u].w[i] = 0;
-    if (h < s.Hkv && sub < lanes_used) {
-      raw[u].load(ip + bytes_of<FI>(h * in.sh));
+    for (int u = 0; u < kSteps; ++u) {
+      const int h = h0 + u * kRowsPerStep;
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) {
+#pragma unroll
+        for (int i = 0; i < Raw8<FI>::kWords; ++i) next[u][v].w[i] = 0;
+        if (h < s.Hkv && exists[v]) next[u][v].load(ip + bytes_of<FI>(ir + h * in.sh + v * kPiece));
+      }
       if constexpr (kQuantized<FI>) {
-        const float* p = in.scales + layer * in.scl + src * in.sct + h * in.sch;
-        if constexpr (FI == KVCRUSH_INT4) sc[u] = __ldg(reinterpret_cast<const float2*>(p)); else sc[u].x = __ldg(p);
+        const float* p = in.scales + sr + h * in.sch;
+        next_sc[u] = make_float2(0.f, 0.f);
+        if (h < s.Hkv) { if constexpr (FI == KVCRUSH_INT4) next_sc[u] = __ldg(reinterpret_cast<const float2*>(p)); else next_sc[u].x = __ldg(p); }
       }
     }
-  }
+  };
+  load(0);
+  for (int r = 0; r < n_rows; ++r) {
+    // the next row is under way while this one is converted
+    const long long orow = __shfl_sync(0xFFFFFFFFu, ob, r), sr = __shfl_sync(0xFFFFFFFFu, sb, r);
+    Raw8<FI> raw[kSteps][kVecs];
+    float2 sc[kSteps];
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u) {
-    const int h = h0 + u * kRowsPerStep;
-    const bool there = h < s.Hkv && sub < lanes_used;
-    float x[8];
-    raw[u].widen(x);
-    if constexpr (kQuantized<FO>) {
-      Raw8<FO> codes;
-      float scale, zero;
-      quantize8<FO, kLanes>(x, lanes_used, codes, scale, zero);
-      if (there) codes.store(op + bytes_of<FO>(h * out.sh));
-      if (there && sub == 0) {
-        float* p = out.scales + layer * out.scl + dst * out.sct + h * out.sch;
-        if constexpr (FO == KVCRUSH_INT4) *reinterpret_cast<float2*>(p) = make_float2(scale, zero); else *p = scale;
+    for (int u = 0; u < kSteps; ++u) {
+      if constexpr (kQuantized<FI>) sc[u] = next_sc[u];
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) raw[u][v] = next[u][v];
+    }
+    if (r + 1 < n_rows) load(r + 1);
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      const int h = h0 + u * kRowsPerStep;
+      float x[kVecs][8];
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) raw[u][v].widen(x[v]);
+      if constexpr (kQuantized<FO>) {
+        Raw8<FO> codes[kVecs];
+        float scale, zero;
+        quantize_row<FO, kLanes, kVecs>(x, exists, codes, scale, zero);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v)
+          if (h < s.Hkv && exists[v]) codes[v].store(op + bytes_of<FO>(orow + h * out.sh + v * kPiece));
+        if (h < s.Hkv && sub == 0) {
+          float* p = out.scales + sr + h * out.sch;
+          if constexpr (FO == KVCRUSH_INT4) *reinterpret_cast<float2*>(p) = make_float2(scale, zero); else *p = scale;
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+          if (h < s.Hkv && exists[v]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[v][i] = FI == KVCRUSH_INT4 ? fmaf(x[v][i], sc[u].x, sc[u].y) : x[v][i] * sc[u].x;
+            Raw8<FO> w;
+            w.narrow(x[v]);
+            w.store(op + bytes_of<FO>(orow + h * out.sh + v * kPiece));
+          }
+        }
       }
-    } else if (there) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = FI == KVCRUSH_INT4 ? fmaf(x[i], sc[u].x, sc[u].y) : x[i] * sc[u].x;
-      Raw8<FO> v;
-      v.narrow(x);
-      v.store(op + bytes_of<FO>(h * out.sh));
     }
   }
 }
 
-template <int FI, int FO, int kLanes>
+template <int FI, int FO, int kLanes, int kVecs>
 int launch_lanes(const Shape& s, ConvertArgs& a, int n_tensors, cudaStream_t stream) {
-  constexpr int heads = kSteps * 32 / kLanes;
-  a.items_per_row = (s.Hkv + heads - 1) / heads;
-  const long long blocks = (a.rows.total * a.items_per_row * n_tensors + kWarps - 1) / kWarps;
+  constexpr int kSteps = kVecs == 1 ? 4 : kVecs == 2 ? 2 : 1, heads = kSteps * 32 / kLanes;
+  a.chunks = (s.Hkv + heads - 1) / heads;
+  // as many rows a warp as leave the chip several times the warps it holds
+  a.rows_per_warp = 1;
+  while (a.rows_per_warp < 16 && a.rows.total * a.chunks * n_tensors > 256LL * sm_count() * a.rows_per_warp) a.rows_per_warp *= 2;
+  const long long groups = (a.rows.total + a.rows_per_warp - 1) / a.rows_per_warp;
+  const long long blocks = (groups * a.chunks * n_tensors + kWarps - 1) / kWarps;
   if (blocks > 0x7FFFFFFFLL) return KVCRUSH_ERR_UNSUPPORTED;
-  return launch_chained(convert_kernel<FI, FO, kLanes>, dim3((unsigned)blocks), dim3(kWarps * 32), 0, stream, 1, s, a, n_tensors);
+  return launch_chained(convert_kernel<FI, FO, kLanes, kVecs, kSteps>, dim3((unsigned)blocks), dim3(kWarps * 32), 0, stream, 1, s, a, n_tensors);
 }
 
+// Lanes and pieces of a row: few lanes with several pieces, so that the row's statistics cost little.
 template <int FI, int FO>
 int launch_formats(const Shape& s, ConvertArgs& a, int n_tensors, cudaStream_t stream) {
-  if (s.D <= 64) return launch_lanes<FI, FO, 8>(s, a, n_tensors, stream);
-  if (s.D <= 128) return launch_lanes<FI, FO, 16>(s, a, n_tensors, stream);
-  return launch_lanes<FI, FO, 32>(s, a, n_tensors, stream);
+  if (s.D <= 32) return launch_lanes<FI, FO, 4, 1>(s, a, n_tensors, stream);
+  if (s.D <= 64) return launch_lanes<FI, FO, 4, 2>(s, a, n_tensors, stream);
+  if (s.D <= 96) return launch_lanes<FI, FO, 4, 3>(s, a, n_tensors, stream);
+  if (s.D <= 128) return launch_lanes<FI, FO, 8, 2>(s, a, n_tensors, stream);
+  if (s.D <= 192) return launch_lanes<FI, FO, 8, 3>(s, a, n_tensors, stream);
+  return launch_lanes<FI, FO, 16, 2>(s, a, n_tensors, stream);
 }
 
 template <int V>
