@@ -2,14 +2,14 @@
 //
 // Bound by reading the cache, which passes through the chip once for every block of 8 to 32 query rows.  A cluster shares one
 // (layer, sequence, KV head) and a block of its query rows (new tokens x query heads of the group); a warp takes tiles of 16
-// keys.  Both products run as mma.sync with the cache as the left operand, which needs no staging of the cache:
-//   logits   S^T[16 keys x 8 rows] = K Q^T: a lane's 16-byte piece of a key row is used as the operand registers of its
-//            steps as it arrives; the channels may come in any order as long as the queries' registers do too
-//   output   O^T[16 channels x 8 rows] += V^T P^T: a lane holds the same channels of four keys and pairs them up with byte
-//            permutations; the weights are turned around by one 8x8 transposition a half tile
-// Codes are used as exact 16-bit integers; a row's scale multiplies the logit, and the weight on the other side, so that no
-// value is ever dequantised.  Weights that carry a scale have a maximum of their own (below), since the largest weight
-// need not belong to the largest product of weight and scale.
+// keys, which it copies ahead into a ring of its own in shared memory (cp.async; rows and channels that do not exist
+// arrive as zeros), so that no warp waits for another.  Both products run as mma.sync with the cache as the left operand:
+//   logits   S^T[16 keys x 8 rows] = K Q^T
+//   output   O^T[16 channels x 8 rows] += V^T P^T, the weights turned around by one 8x8 transposition a half tile
+// 16-bit values become operands by ldmatrix.  Codes are used as exact half-precision integers: the channels of a product may
+// come in any order, so a lane takes whole words of codes and pairs them up by byte permutations; a row's scale multiplies the
+// logit, and the weight on the other side, so that no value is ever dequantised.  Weights that carry a scale have a
+// maximum of their own (below), since the largest weight need not belong to the largest product of weight and scale.
 #pragma once
 
 #include <atomic>
@@ -83,19 +83,12 @@ struct Layout {
   __device__ static __forceinline__ int k_channel(int piece, int c) { return (piece * 4 + c) * kChannels; }
   __device__ static __forceinline__ int v_channel(int piece, int g) { return (piece * 8 + g) * kVChannels; }
   // first of the two channels of m-tile mt that lane g holds (rows g and g + 8 of the operand)
-  __device__ static __forceinline__ int out_channel(int mt, int g) { return v_channel(mt / (kVChannels / 2), g) + 2 * (mt % (kVChannels / 2)); }
-};
-
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char* p, bool there) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = 0u;
-  if (there) {
-    if constexpr (N == 4) { const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p)); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
-    else if constexpr (N == 2) { const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p)); w[0] = v.x; w[1] = v.y; }
-    else w[0] = __ldcs(reinterpret_cast<const unsigned int*>(p));
+  // (16-bit values come through ldmatrix: channels g and g + 8 of sixteen)
+  static constexpr int kPairStep = kBits == 16 ? 8 : 1;
+  __device__ static __forceinline__ int out_channel(int mt, int g) {
+    return kBits == 16 ? 16 * mt + g : v_channel(mt / (kVChannels / 2), g) + 2 * (mt % (kVChannels / 2));
   }
-}
+};
 
 // Where a tile's rows are: row numbers of its two halves of eight keys, and how many of each exist.
 struct Halves {
@@ -112,92 +105,148 @@ template <class T> __device__ __forceinline__ const T* at_row(const T* base, int
   return base + (unsigned long long)(uint32_t)row * stride;
 }
 
+// Operand pairs of a word of a key row: two channels each.
+template <int F>
+__device__ __forceinline__ void key_pairs(uint32_t w, uint32_t (&p)[16 / Bits<F>::value]) {
+  if constexpr (F == KVCRUSH_INT8) { p[0] = int8_half2<false>(w ^ 0x80808080u); p[1] = int8_half2<true>(w ^ 0x80808080u); }
+  else if constexpr (F == KVCRUSH_E4M3) { p[0] = e4m3_half2(w & 0xFFFFu); p[1] = e4m3_half2(w >> 16); }
+  else { p[0] = int4_half2<0>(w); p[1] = int4_half2<1>(w); p[2] = int4_half2<2>(w); p[3] = int4_half2<3>(w); }
+}
+// Operand pairs (key a, key b) of the channels of a word of both keys' value rows.
+template <int F>
+__device__ __forceinline__ void value_pairs(uint32_t wa, uint32_t wb, uint32_t (&p)[32 / Bits<F>::value]) {
+  if constexpr (F == KVCRUSH_INT8) {
+    const uint32_t lo = __byte_perm(wa, wb, 0x5140) ^ 0x80808080u, hi = __byte_perm(wa, wb, 0x7362) ^ 0x80808080u;
+    p[0] = int8_half2<false>(lo); p[1] = int8_half2<true>(lo); p[2] = int8_half2<false>(hi); p[3] = int8_half2<true>(hi);
+  } else if constexpr (F == KVCRUSH_E4M3) {
+    const uint32_t lo = __byte_perm(wa, wb, 0x5140), hi = __byte_perm(wa, wb, 0x7362);
+    p[0] = e4m3_half2(lo & 0xFFFFu); p[1] = e4m3_half2(lo >> 16); p[2] = e4m3_half2(hi & 0xFFFFu); p[3] = e4m3_half2(hi >> 16);
+  } else {
+    const uint32_t lo = __byte_perm(wa, wb, 0x5410), hi = __byte_perm(wa, wb, 0x7632);
+    p[0] = int4_half2<0>(lo); p[1] = int4_half2<1>(lo); p[2] = int4_half2<2>(lo); p[3] = int4_half2<3>(lo);
+    p[4] = int4_half2<0>(hi); p[5] = int4_half2<1>(hi); p[6] = int4_half2<2>(hi); p[7] = int4_half2<3>(hi);
+  }
+}
+
+// ---- a tile in shared memory -------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16_ahead(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// kBytes of 4, 8 or 16; nothing is read and zeros are written unless there
+template <int kBytes>
+__device__ __forceinline__ void copy_ahead(uint32_t dst, const void* src, bool there) {
+  const int n = there ? kBytes : 0;
+  if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(n) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <bool kTrans>
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  if constexpr (kTrans) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+  else asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void shared_words(uint32_t (&w)[N], uint32_t addr) {
+  if constexpr (N == 4) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+  else if constexpr (N == 2) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr) : "memory");
+  else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(addr) : "memory");
+}
+
+// Keys, then values, 16 rows each, then their scales.  Rows of 128 bytes or more have their 16-byte chunks permuted so that
+// neither product's reads meet in a bank; shorter ones are 16 bytes apart.
 template <int F, int DP>
-struct KeyTile {
-  using L = Layout<F, DP>;
-  uint32_t a[2][L::kPieces][L::kWords];      // keys g and g + 8
-  float2 sc[2];                              // scale (and zero)
-  // kFull: all 16 keys exist
+struct Stage {
+  static constexpr int kRowBytes = DP * Bits<F>::value / 8, kChunks = kRowBytes / 16;
+  static constexpr bool kPermuted = kRowBytes >= 128;
+  static constexpr int kPitch = kPermuted ? kRowBytes : kRowBytes + 16, kTileBytes = kTile * kPitch;
+  static constexpr int kScaleBytes = F == KVCRUSH_INT4 ? 8 : 4;
+  static constexpr int kScales = 2 * kTileBytes, kBytes = kScales + (kQuantized<F> ? 2 * kTile * kScaleBytes : 0);
+  // 16-bit rows are read eight rows to a chunk; codes by pairs of rows (keys) and by every other row (values)
+  __device__ static constexpr int permutation(int row) { return !kPermuted ? 0 : kQuantized<F> ? (row & 6) ^ (row & 1) << 2 : row & 7; }
+  __device__ static __forceinline__ uint32_t at(int row, int chunk) { return (uint32_t)(row * kPitch + (chunk ^ permutation(row)) * 16); }
+
+  // A lane copies the same chunk of every kRowsPerCopy-th row.
+  static constexpr int kRowsPerCopy = 32 / kChunks;
+  struct Lane {
+    const unsigned char *k, *v;              // its chunk of its first row
+    const float* scales;                     // lanes 0 .. 15: of the keys, 16 .. 31: of the values
+    uint32_t k_st, v_st, scale_st;           // strides
+    uint32_t dst;                            // where its first row goes, without the chunk
+    int chunk;                               // permuted as in its first row
+    bool used;                               // the head has these channels
+  };
+  static __device__ __forceinline__ Lane lane_of(const Source& s, int D, int lane) {
+    Lane l;
+    const int row = lane / kChunks, chunk = lane % kChunks;
+    l.k = at_row(s.k, row, s.k_st) + chunk * 16;
+    l.v = at_row(s.v, row, s.v_st) + chunk * 16;
+    l.k_st = s.k_st; l.v_st = s.v_st;
+    l.scales = lane < 16 ? s.ks : s.vs;
+    l.scale_st = lane < 16 ? s.k_sct : s.v_sct;
+    l.dst = row * kPitch;
+    l.chunk = chunk ^ permutation(row & 7);
+    l.used = chunk * 16 < (int)bytes_of<F>(D);
+    return l;
+  }
+  // kFull: all 16 rows exist; otherwise zeros take the place of those that do not.
   template <bool kFull>
-  __device__ __forceinline__ void load(const Source& s, const Halves& h, int D, int lane) {
-    const int g = lane >> 2, c = lane & 3;
+  static __device__ __forceinline__ void fetch(uint32_t stage, const Lane& l, const Halves& h, int lane) {
+    if (l.used) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const bool there = kFull || g < h.n[j];
-      const unsigned char* p = at_row(s.k, h.row[j] + g, s.k_st);
+      for (int kv = 0; kv < 2; ++kv) {
+        const unsigned char* base = kv ? l.v : l.k;
+        const uint32_t stride = kv ? l.v_st : l.k_st;
+        const uint32_t to = stage + kv * kTileBytes + l.dst;
+        const unsigned char* p = base;
 #pragma unroll
-      for (int i = 0; i < L::kPieces; ++i) load_words(a[j][i], p + bytes_of<F>(L::k_channel(i, c)), there && L::k_channel(i, c) < D);
-      if constexpr (kQuantized<F>) {
-        sc[j] = make_float2(0.f, 0.f);
-        const float* sp = at_row(s.ks, h.row[j] + g, s.k_sct);
-        if (there) { if (F == KVCRUSH_INT4) sc[j] = __ldg(reinterpret_cast<const float2*>(sp)); else sc[j].x = __ldg(sp); }
+        for (int i = 0; i < kTile / kRowsPerCopy; ++i) {
+          const int first = i * kRowsPerCopy;                        // of the rows of this copy
+          if (kRowsPerCopy == 16) p = at_row(base, lane / kChunks < 8 ? h.row[0] : h.row[1] - 8, stride);
+          else if (first % 8 == 0) p = at_row(base, h.row[first / 8], stride);
+          const uint32_t dst = to + first * kPitch + ((l.chunk ^ permutation(first & 7)) << 4);
+          if (kFull) {
+            copy16_ahead(dst, p);
+          } else {
+            const int row = lane / kChunks + first;
+            const bool there = (row & 7) < (row < 8 ? h.n[0] : h.n[1]);
+            copy_ahead<16>(dst, there ? p : base, there);
+          }
+          p += (unsigned long long)kRowsPerCopy * stride;
+        }
       }
-    }
-  }
-  // Operand pairs of word i of a piece: two channels each.
-  __device__ static __forceinline__ void pairs(uint32_t w, uint32_t (&p)[32 / L::kBits / 2]) {
-    if constexpr (F == KVCRUSH_INT8) { p[0] = int8_half2<false>(w ^ 0x80808080u); p[1] = int8_half2<true>(w ^ 0x80808080u); }
-    else if constexpr (F == KVCRUSH_E4M3) { p[0] = e4m3_half2(w & 0xFFFFu); p[1] = e4m3_half2(w >> 16); }
-    else if constexpr (F == KVCRUSH_INT4) { p[0] = int4_half2<0>(w); p[1] = int4_half2<1>(w); p[2] = int4_half2<2>(w); p[3] = int4_half2<3>(w); }
-    else p[0] = w;
-  }
-};
-// FO: whose layout the output has.  Values of another type than the cache's (those of new tokens, 16-bit) are loaded eight
-// channels at a time from where the cache's layout has them.
-template <int F, int DP, int FO = F>
-struct ValueTile {
-  using L = Layout<F, DP>;
-  __device__ static __forceinline__ int channel(int piece, int g) {
-    if constexpr (F == FO) return L::v_channel(piece, g);
-    else return Layout<FO, DP>::out_channel(4 * piece, g);
-  }
-  uint32_t a[4][L::kVPieces][L::kVWords];    // keys 2c, 2c + 1, 2c + 8, 2c + 9
-  float2 sc[2];                              // keys g and g + 8
-  template <bool kFull>
-  __device__ __forceinline__ void load(const Source& s, const Halves& h, int D, int lane) {
-    const int g = lane >> 2, c = lane & 3;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool there = kFull || 2 * c + (j & 1) < h.n[j >> 1];
-      const unsigned char* p = at_row(s.v, h.row[j >> 1] + 2 * c + (j & 1), s.v_st);
-#pragma unroll
-      for (int i = 0; i < L::kVPieces; ++i) load_words(a[j][i], p + bytes_of<F>(channel(i, g)), there && channel(i, g) < D);
     }
     if constexpr (kQuantized<F>) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        sc[j] = make_float2(0.f, 0.f);
-        const float* sp = at_row(s.vs, h.row[j] + g, s.v_sct);
-        if (kFull || g < h.n[j]) { if (F == KVCRUSH_INT4) sc[j] = __ldg(reinterpret_cast<const float2*>(sp)); else sc[j].x = __ldg(sp); }
-      }
+      const int row = lane & 15, first = row < 8 ? h.row[0] : h.row[1] - 8;
+      const bool there = kFull || (row & 7) < (row < 8 ? h.n[0] : h.n[1]);
+      copy_ahead<kScaleBytes>(stage + kScales + lane * kScaleBytes, there ? at_row(l.scales, first + row, l.scale_st) : l.scales, there);
     }
   }
-  // Operand pairs (key a, key b) of the channels of word i of both keys.
-  __device__ static __forceinline__ void pairs(uint32_t wa, uint32_t wb, uint32_t (&p)[32 / L::kBits]) {
-    if constexpr (F == KVCRUSH_INT8) {
-      const uint32_t lo = __byte_perm(wa, wb, 0x5140) ^ 0x80808080u, hi = __byte_perm(wa, wb, 0x7362) ^ 0x80808080u;
-      p[0] = int8_half2<false>(lo); p[1] = int8_half2<true>(lo); p[2] = int8_half2<false>(hi); p[3] = int8_half2<true>(hi);
-    } else if constexpr (F == KVCRUSH_E4M3) {
-      const uint32_t lo = __byte_perm(wa, wb, 0x5140), hi = __byte_perm(wa, wb, 0x7362);
-      p[0] = e4m3_half2(lo & 0xFFFFu); p[1] = e4m3_half2(lo >> 16); p[2] = e4m3_half2(hi & 0xFFFFu); p[3] = e4m3_half2(hi >> 16);
-    } else if constexpr (F == KVCRUSH_INT4) {
-      const uint32_t lo = __byte_perm(wa, wb, 0x5410), hi = __byte_perm(wa, wb, 0x7632);
-      p[0] = int4_half2<0>(lo); p[1] = int4_half2<1>(lo); p[2] = int4_half2<2>(lo); p[3] = int4_half2<3>(lo);
-      p[4] = int4_half2<0>(hi); p[5] = int4_half2<1>(hi); p[6] = int4_half2<2>(hi); p[7] = int4_half2<3>(hi);
-    } else {
-      p[0] = __byte_perm(wa, wb, 0x5410); p[1] = __byte_perm(wa, wb, 0x7632);
-    }
+  // scale (and zero) of keys or values row `row`
+  static __device__ __forceinline__ float2 scale(uint32_t stage, bool values, int row) {
+    float2 v = make_float2(0.f, 0.f);
+    const uint32_t p = stage + kScales + (values ? kTile + row : row) * kScaleBytes;
+    if constexpr (F == KVCRUSH_INT4) asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(p) : "memory");
+    else asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v.x) : "r"(p) : "memory");
+    return v;
   }
 };
 
-// One channel of a value row, codes without their scale (INT4: less 8).
-template <int F>
-__device__ __forceinline__ float value_at(const unsigned char* row, int channel) {
-  if constexpr (F == KVCRUSH_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[channel]);
-  else if constexpr (F == KVCRUSH_FP16) return __half2float(reinterpret_cast<const __half*>(row)[channel]);
-  else if constexpr (F == KVCRUSH_INT8) return (float)reinterpret_cast<const signed char*>(row)[channel];
-  else if constexpr (F == KVCRUSH_E4M3) return __low2float(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)row[channel], __NV_E4M3)));
-  else return (float)(int)((row[channel >> 1] >> (4 * (channel & 1))) & 15) - 8.f;
+// One channel of row `row` of the values at `tile`; codes without their scale (INT4: less 8).
+template <int F, int DP>
+__device__ __forceinline__ float value_at(uint32_t tile, int row, int channel) {
+  using T = Stage<F, DP>;
+  const int byte = channel * Bits<F>::value / 8;
+  uint32_t w[1];
+  shared_words(w, tile + T::at(row, byte >> 4) + (byte & 12));
+  if constexpr (F == KVCRUSH_BF16) return (channel & 1) ? unpack_bf16(w[0]).y : unpack_bf16(w[0]).x;
+  else if constexpr (F == KVCRUSH_FP16) return (channel & 1) ? unpack_fp16(w[0]).y : unpack_fp16(w[0]).x;
+  else if constexpr (F == KVCRUSH_INT8) return (float)(int)(signed char)(w[0] >> (8 * (channel & 3)));
+  else if constexpr (F == KVCRUSH_E4M3) return unpack_fp16(e4m3_half2(w[0] >> (8 * (channel & 3)) & 0xFFu)).x;
+  else return (float)(int)(w[0] >> (4 * (channel & 7)) & 15u) - 8.f;
 }
 // Is any of the four numbers (or two, of 16 bits) of a word not finite?
 template <int F>
@@ -226,67 +275,152 @@ struct Running {
   float o[NB][DP / 16][4];
 };
 
-// Queries as operands of the logits: rows of `stride` bytes in shared memory, in the order of the cache's channels.
+constexpr float kSlack = 8.f;
+
+// Queries as operands: rows of `stride` bytes in shared memory, in the order of the cache's channels.
 struct Queries {
-  const unsigned char* sh;
+  uint32_t sh;
   int stride;
 };
 
-// Multiplies a tile of keys with 8 NB query rows.
+// Multiplies a tile of keys with 8 NB query rows.  kRegs: the queries' operands are in qr, otherwise in shared memory.
 template <int F, int A, int DP, int NB, bool kRegs, int kQRegs>
-__device__ __forceinline__ void logits(const KeyTile<F, DP>& K, const Queries& q, const uint32_t (&qr)[kQRegs], int lane, float (&x)[NB][4]) {
+__device__ __forceinline__ void logits(uint32_t stage, const Queries& q, const uint32_t (&qr)[kQRegs], int lane, float (&x)[NB][4]) {
   using L = Layout<F, DP>;
-  constexpr int kPairs = 32 / L::kBits / 2 < 1 ? 1 : 32 / L::kBits / 2;   // of a word
+  using T = Stage<F, DP>;
   const int g = lane >> 2, c = lane & 3;
+  float y[NB][4];                            // a second chain of sums: half the latency
 #pragma unroll
   for (int n = 0; n < NB; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[n][i] = 0.f;
+    for (int i = 0; i < 4; ++i) x[n][i] = y[n][i] = 0.f;
+  if constexpr (!kQuantized<F>) {
+    const int key = lane & 15;
 #pragma unroll
-  for (int i = 0; i < L::kPieces; ++i) {
-    uint32_t pa[L::kChannels / 2], pb[L::kChannels / 2];
+    for (int i = 0; i < DP / 32; ++i) {      // 32 channels: two steps
+      uint32_t a[2][4];
 #pragma unroll
-    for (int w = 0; w < L::kWords; ++w) {
-      uint32_t p[kPairs], r[kPairs];
-      KeyTile<F, DP>::pairs(K.a[0][i][w], p);
-      KeyTile<F, DP>::pairs(K.a[1][i][w], r);
+      for (int j = 0; j < 2; ++j) ldmatrix4<false>(a[j], stage + T::at(key, 4 * i + 2 * j + (lane >> 4)));
 #pragma unroll
-      for (int j = 0; j < kPairs; ++j) { pa[w * kPairs + j] = p[j]; pb[w * kPairs + j] = r[j]; }
-    }
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-#pragma unroll
-      for (int e = 0; e < L::kChannels / 8; ++e) {                   // eight channels: two steps
+      for (int n = 0; n < NB; ++n) {
         uint32_t b[4];
         if constexpr (kRegs) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) b[j] = qr[((n * L::kPieces + i) * (L::kChannels / 8) + e) * 4 + j];
+          for (int j = 0; j < 4; ++j) b[j] = qr[(n * (DP / 32) + i) * 4 + j];
         } else {
-          const uint4 v = *reinterpret_cast<const uint4*>(q.sh + (n * 8 + g) * q.stride + (L::k_channel(i, c) + 8 * e) * 2);
-          b[0] = v.x; b[1] = v.y; b[2] = v.z; b[3] = v.w;
+          ldmatrix4<false>(b, q.sh + (n * 8 + (lane & 7)) * q.stride + (4 * i + (lane >> 3)) * 16);
         }
-        mma<A>(x[n], pa[4 * e], pb[4 * e], pa[4 * e + 1], pb[4 * e + 1], b[0], b[1]);
-        mma<A>(x[n], pa[4 * e + 2], pb[4 * e + 2], pa[4 * e + 3], pb[4 * e + 3], b[2], b[3]);
+        mma<A>(x[n], a[0][0], a[0][1], a[0][2], a[0][3], b[0], b[1]);
+        mma<A>(y[n], a[1][0], a[1][1], a[1][2], a[1][3], b[2], b[3]);
+      }
+    }
+  } else {
+    constexpr int kPairs = 32 / L::kBits / 2;                        // of a word
+#pragma unroll
+    for (int i = 0; i < L::kPieces; ++i) {
+      uint32_t wa[L::kWords], wb[L::kWords], pa[L::kChannels / 2], pb[L::kChannels / 2];
+      const int byte = (int)bytes_of<F>(L::k_channel(i, c));
+      shared_words(wa, stage + T::at(g, byte >> 4) + (byte & 15));
+      shared_words(wb, stage + T::at(g + 8, byte >> 4) + (byte & 15));
+#pragma unroll
+      for (int w = 0; w < L::kWords; ++w) {
+        uint32_t p[kPairs], r[kPairs];
+        key_pairs<F>(wa[w], p);
+        key_pairs<F>(wb[w], r);
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) { pa[w * kPairs + j] = p[j]; pb[w * kPairs + j] = r[j]; }
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+#pragma unroll
+        for (int e = 0; e < L::kChannels / 8; ++e) {                 // eight channels: two steps
+          uint32_t b[4];
+          if constexpr (kRegs) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = qr[((n * L::kPieces + i) * (L::kChannels / 8) + e) * 4 + j];
+          } else {
+            shared_words(b, q.sh + (n * 8 + g) * q.stride + (L::k_channel(i, c) + 8 * e) * 2);
+          }
+          mma<A>(x[n], pa[4 * e], pb[4 * e], pa[4 * e + 1], pb[4 * e + 1], b[0], b[1]);
+          mma<A>(y[n], pa[4 * e + 2], pb[4 * e + 2], pa[4 * e + 3], pb[4 * e + 3], b[2], b[3]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NB; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[n][i] += y[n][i];
+}
+
+// The tile's values as operands: for every m-tile use(t, four operand registers).
+template <int F, int DP, class Use>
+__device__ __forceinline__ void value_operands(uint32_t stage, int lane, Use&& use) {
+  using L = Layout<F, DP>;
+  using T = Stage<F, DP>;
+  const uint32_t values = stage + T::kTileBytes;
+  if constexpr (!kQuantized<F>) {
+    const int key = (lane & 7) + (lane >> 4) * 8;
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) {
+      uint32_t a[4];
+      ldmatrix4<true>(a, values + T::at(key, 2 * t + (lane >> 3 & 1)));
+      use(t, a[0], a[1], a[2], a[3]);
+    }
+  } else {
+    constexpr int kPairs = 32 / L::kBits;
+    const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int i = 0; i < L::kVPieces; ++i) {
+      uint32_t w[4][L::kVWords];
+      const int byte = (int)bytes_of<F>(L::v_channel(i, g));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) shared_words(w[j], values + T::at(2 * c + (j & 1) + (j >> 1) * 8, byte >> 4) + (byte & 15));
+#pragma unroll
+      for (int k = 0; k < L::kVWords; ++k) {
+        uint32_t p[kPairs], r[kPairs];
+        value_pairs<F>(w[0][k], w[1][k], p);
+        value_pairs<F>(w[2][k], w[3][k], r);
+#pragma unroll
+        for (int j = 0; j < kPairs; j += 2) use(((i * L::kVWords + k) * kPairs + j) / 2, p[j], p[j + 1], r[j], r[j + 1]);
       }
     }
   }
 }
+// 16-bit values for an output in the layout of a quantised cache FO.
+template <int F, int FO, int DP, class Use>
+__device__ __forceinline__ void value_operands_like(uint32_t stage, int lane, Use&& use) {
+  using T = Stage<F, DP>;
+  const uint32_t values = stage + T::kTileBytes;
+  const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) {
+    uint32_t w[4][1];
+    const int byte = Layout<FO, DP>::out_channel(t, g) * 2;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) shared_words(w[j], values + T::at(2 * c + (j & 1) + (j >> 1) * 8, byte >> 4) + (byte & 15));
+    use(t, __byte_perm(w[0][0], w[1][0], 0x5410), __byte_perm(w[0][0], w[1][0], 0x7632), __byte_perm(w[2][0], w[3][0], 0x5410),
+        __byte_perm(w[2][0], w[3][0], 0x7632));
+  }
+}
 
-// Adds a tile to the running state.  x: logits (log2 domain), -inf where a key is not seen (then `hidden`, bit 4 n + i, says
-// so); F, A: the tile's type and the type it is multiplied in; kScaled: the state's output has a maximum of its own;
-// kFull: every key exists and is seen by all rows.  Maxima start at the lowest finite number, so that a logit of -inf
-// has weight 0 whatever came before.
-template <int F, int FO, int A, int DP, int NB, bool kScaled, bool kFull>
-__device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const Source& src, const Halves& h, int D, float (&x)[NB][4], uint32_t hidden,
-                                         bool masked, Running<NB, DP, kScaled>& run, int lane) {
-  using L = Layout<F, DP>;
+// Adds a tile to the running state.  x: logits (log2 domain), -inf where a key is not seen (then bit 4 n + i of `hidden` says
+// so); F, A: the tile's type and the type it is multiplied in; FO: the cache's type, whose layout the output has.  Maxima
+// start at the lowest finite number, so that a logit of -inf has weight 0 whatever came before.
+template <int F, int FO, int A, int DP, int NB>
+__device__ __forceinline__ void add_tile(uint32_t stage, const Halves& h, int D, float (&x)[NB][4], uint32_t hidden,
+                                         Running<NB, DP, kQuantized<FO>>& run, int lane) {
+  constexpr bool kScaled = kQuantized<FO>;
+  using T = Stage<F, DP>;
+  const int g = lane >> 2;
   // log2 of the value rows' scales
   float lv[2] = {0.f, 0.f}, vz[2] = {0.f, 0.f};
   if constexpr (kQuantized<F>) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      lv[j] = __log2f(V.sc[j].x);
-      if (F == KVCRUSH_INT4) vz[j] = fmaf(8.f, V.sc[j].x, V.sc[j].y);
+      const float2 sc = T::scale(stage, true, g + 8 * j);
+      lv[j] = __log2f(sc.x);
+      if (F == KVCRUSH_INT4) vz[j] = fmaf(8.f, sc.x, sc.y);
     }
   }
   float d[NB][4], d2[NB][4];
@@ -300,14 +434,15 @@ __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const So
       }
   };
   differences();
-  // The maximum of a row seldom moves: the reduction over the tile's keys is done where any lane has a larger logit.
+  // Weights may exceed 1: what they are relative to moves only where a logit is kSlack above it (in the log2 domain; half
+  // precision holds weights up to 2^15).  Most tiles after the first leave it alone.
   float most = 0.f;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     most = fmaxf(fmaxf(most, fmaxf(d[n][0], d[n][1])), fmaxf(d[n][2], d[n][3]));
     if (kScaled) most = fmaxf(fmaxf(most, fmaxf(d2[n][0], d2[n][1])), fmaxf(d2[n][2], d2[n][3]));
   }
-  if (__any_sync(kAll, most > 0.f)) {
+  if (__any_sync(kAll, most > kSlack)) {
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -333,6 +468,14 @@ __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const So
       }
     differences();
   }
+  const bool masked = __any_sync(kAll, hidden != 0u);
+  if (kScaled && masked) {                             // a scale that is NaN stays with the rows that see it
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (hidden >> (4 * n + i) & 1u) d2[n][i] = neg_inf();
+  }
   uint32_t b0[NB], b1[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
@@ -340,33 +483,33 @@ __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const So
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float p = ex2(d[n][i]);
-      const bool unseen = !kFull && (hidden >> (4 * n + i) & 1u);
       run.l[n][i & 1] += p;
       w[i] = p;
       if constexpr (kScaled) {
-        if (F == KVCRUSH_INT4) run.b[n][i & 1] = fmaf(p, unseen ? 0.f : vz[i >> 1], run.b[n][i & 1]);
-        w[i] = kQuantized<F> && unseen ? 0.f : ex2(d2[n][i]);
+        if (F == KVCRUSH_INT4 && p != 0.f) run.b[n][i & 1] = fmaf(p, vz[i >> 1], run.b[n][i & 1]);
+        w[i] = ex2(d2[n][i]);
       }
     }
     x[n][0] = w[0]; x[n][1] = w[1]; x[n][2] = w[2]; x[n][3] = w[3];
     b0[n] = transpose8x8(A == KVCRUSH_BF16 ? pack_bf16(w[0], w[1]) : pack_fp16(w[0], w[1]));
     b1[n] = transpose8x8(A == KVCRUSH_BF16 ? pack_bf16(w[2], w[3]) : pack_fp16(w[2], w[3]));
   }
-  if (!kFull && masked) {
+  if (masked) {
     // A weight of 0 takes a value that is not finite along: where there is one, every row adds up the keys that it sees.
     bool bad = false;
+    for (uint32_t e = lane * 16; e < (uint32_t)T::kTileBytes; e += 512) {
+      uint32_t v[4];
+      if (T::kPermuted || (int)(e % T::kPitch) < T::kRowBytes) {     // not the space between rows
+        shared_words(v, stage + T::kTileBytes + e);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < L::kVPieces; ++i)
-#pragma unroll
-        for (int k = 0; k < L::kVWords; ++k) bad |= not_finite<F>(V.a[j][i][k]);
+        for (int k = 0; k < 4; ++k) bad |= not_finite<F>(v[k]);
+      }
+    }
     if (__any_sync(kAll, bad)) {
-      const int g = lane >> 2, c = lane & 3;
+      const int c = lane & 3;
 #pragma unroll 1
       for (int key = 0; key < kTile; ++key) {
         if ((key & 7) >= h.n[key >> 3]) continue;
-        const unsigned char* row = at_row(src.v, h.row[key >> 3] + (key & 7), src.v_st);
         const uint32_t hid = __shfl_sync(kAll, hidden, (key & 7) * 4 + c);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
@@ -380,35 +523,26 @@ __device__ __forceinline__ void add_tile(const ValueTile<F, DP, FO>& V, const So
           for (int t = 0; t < DP / 16; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int ch = Layout<FO, DP>::out_channel(t, g) + (i >> 1);
+              const int ch = Layout<FO, DP>::out_channel(t, g) + (i >> 1) * Layout<FO, DP>::kPairStep;
               const bool unseen = hid >> (4 * n + (key < 8 ? 0 : 2) + (i & 1)) & 1u;
-              if (ch < D && !unseen) run.o[n][t][i] = fmaf(w[i & 1], value_at<F>(row, ch), run.o[n][t][i]);
+              if (ch < D && !unseen) run.o[n][t][i] = fmaf(w[i & 1], value_at<F, DP>(stage + T::kTileBytes, key, ch), run.o[n][t][i]);
             }
         }
       }
       return;
     }
   }
+  auto multiply = [&](int t, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-  for (int i = 0; i < L::kVPieces; ++i)
-#pragma unroll
-    for (int k = 0; k < L::kVWords; ++k) {
-      constexpr int kPairs = 32 / L::kBits;
-      uint32_t p[kPairs], r[kPairs];
-      ValueTile<F, DP, FO>::pairs(V.a[0][i][k], V.a[1][i][k], p);
-      ValueTile<F, DP, FO>::pairs(V.a[2][i][k], V.a[3][i][k], r);
-#pragma unroll
-      for (int j = 0; j < kPairs; j += 2) {
-        const int t = ((i * L::kVWords + k) * kPairs + j) / 2;
-#pragma unroll
-        for (int n = 0; n < NB; ++n) mma<A>(run.o[n][t], p[j], p[j + 1], r[j], r[j + 1], b0[n], b1[n]);
-      }
-    }
+    for (int n = 0; n < NB; ++n) mma<A>(run.o[n][t], a0, a1, a2, a3, b0[n], b1[n]);
+  };
+  if constexpr (F == FO) value_operands<F, DP>(stage, lane, multiply);
+  else value_operands_like<F, FO, DP>(stage, lane, multiply);
 }
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------
 
-// Byte offsets in dynamic shared memory.
+// Byte offsets in dynamic shared memory.  The warps' outputs take the place of the rings at the end.
 template <int F, int FQ, int DP, int NB, int kWarps>
 struct Mem {
   static constexpr int kRows = 8 * NB;
@@ -418,8 +552,16 @@ struct Mem {
   static constexpr int kRowScale = kQNew + kRows * kQStride;                      // [kRows] factor and sum of the queries
   static constexpr int kPart = kRowScale + kRows * 8;                             // [kWarps + 1][kRows] Part
   static constexpr int kFactor = kPart + (kWarps + 1) * kRows * (int)sizeof(Part);
-  static constexpr int kO = (kFactor + kRows * (kMaxCluster + 1) * 4 + 15) / 16 * 16;
-  static constexpr int kEnd = kO + kWarps * kRows * kOStride * 4;
+  static constexpr int kRing = (kFactor + kRows * (kMaxCluster + 1) * 4 + 127) / 128 * 128;
+  static constexpr int kO = kRing;
+  // 96 KB of rings a block: as many stages as fit, two at least, and room for a tile of 16-bit new tokens
+  static constexpr int kStageBytes = (Stage<F, DP>::kBytes + 127) / 128 * 128;
+  static constexpr int kWarpBytes = 96 * 1024 / kWarps;
+  static constexpr int kStages = kWarpBytes / kStageBytes < 2 ? 2 : kWarpBytes / kStageBytes > 6 ? 6 : kWarpBytes / kStageBytes;
+  static constexpr int kNewBytes = kQuantized<F> ? Stage<FQ, DP>::kBytes : 0;
+  static constexpr int kRingBytes = kStages * kStageBytes > kNewBytes ? kStages * kStageBytes : kNewBytes;
+  static constexpr int kOBytes = kWarps * kRows * kOStride * 4;
+  static constexpr int kEnd = kRing + (kWarps * kRingBytes > kOBytes ? kWarps * kRingBytes : kOBytes);
 };
 
 template <int F, int FQ, int DP, int NB, int kWarps, int kBlocks, bool kPages>
@@ -429,10 +571,8 @@ attend_kernel(AttendArgs a) {
   using L = Layout<F, DP>;
   constexpr bool kScaled = kQuantized<F>;
   constexpr int A = kArith<F, FQ>, kRows = M::kRows;
-  // Keys of a tile that take few registers are loaded a tile ahead; otherwise other warps' loads fill the time.
-  constexpr bool kAhead = DP * Bits<F>::value <= 1024;
-  constexpr bool kRegs = NB * DP <= 128 && kAhead;             // queries in registers
-  extern __shared__ __align__(16) unsigned char sh[];
+  constexpr bool kRegs = NB * DP <= 128;                       // queries in registers
+  extern __shared__ __align__(128) unsigned char sh[];
   chain_wait();
   chain_trigger();
   cg::cluster_group cluster = cg::this_cluster();
@@ -448,53 +588,137 @@ attend_kernel(AttendArgs a) {
     n_chosen = choose_pages<FQ, kWarps * 32>(a, w, cluster, n_blk, rank, pages);
   }
   float2* row_scale = reinterpret_cast<float2*>(sh + M::kRowScale);
-  // queries: a warp takes a row
-  for (int r = warp; r < kRows; r += kWarps) {
-    const unsigned char* q = static_cast<const unsigned char*>(a.Q.ptr);
-    if (r < w.rows) q += bytes_of<FQ>(w.layer * a.Q.sl + (w.first + w.token(s.G, r)) * a.Q.st + (w.hk * s.G + w.head(s.G, r)) * a.Q.sh);
-    float v[DP / 32], big = 0.f, sum = 0.f;
+  const Source src{static_cast<const unsigned char*>(a.K.ptr) + bytes_of<F>(w.layer * a.K.sl + w.hk * a.K.sh),
+                   static_cast<const unsigned char*>(a.V.ptr) + bytes_of<F>(w.layer * a.V.sl + w.hk * a.V.sh),
+                   (uint32_t)bytes_of<F>(a.K.st), (uint32_t)bytes_of<F>(a.V.st), a.K.scales + w.layer * a.K.scl + w.hk * a.K.sch,
+                   a.V.scales + w.layer * a.V.scl + w.hk * a.V.sch, (uint32_t)a.K.sct, (uint32_t)a.V.sct};
+  Source fresh{};
+  if (!kPages && w.own)
+    fresh = Source{static_cast<const unsigned char*>(a.K_new.ptr) + bytes_of<FQ>(w.layer * a.K_new.sl + w.hk * a.K_new.sh),
+                   static_cast<const unsigned char*>(a.V_new.ptr) + bytes_of<FQ>(w.layer * a.V_new.sl + w.hk * a.V_new.sh),
+                   (uint32_t)bytes_of<FQ>(a.K_new.st), (uint32_t)bytes_of<FQ>(a.V_new.st), nullptr, nullptr, 0, 0};
+  const int halves_per_page = kPages ? a.pages.page_size / 8 : 1;
+  const uint32_t page_magic = kPages && halves_per_page > 1 ? 0xFFFFFFFFu / (uint32_t)halves_per_page + 1u : 0u;
+  const int cached = kPages ? (n_chosen * halves_per_page + 1) / 2 : (w.seen + kTile - 1) / kTile;
+  const int n_tiles = cached + (w.own + kTile - 1) / kTile;
+  const int per = (n_tiles + n_blk - 1) / n_blk, lo = min(n_tiles, rank * per), hi = min(n_tiles, lo + per);
+  // tiles whose keys all exist and are seen by every query row; of the chosen pages only the last may be short
+  int full;
+  if (kPages) {
+    const int last = n_chosen ? pages.chosen[n_chosen - 1] : 0;
+    full = n_chosen ? ((n_chosen - 1) * a.pages.page_size + min(a.pages.page_size, w.seen - last * a.pages.page_size)) / kTile : 0;
+  } else {
+    full = (w.own ? w.seen : w.limit(s.G, 0)) / kTile;
+  }
+  auto halves = [&](int t) {
+    Halves h;
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
-      const int d = 32 * i + lane;
-      v[i] = r < w.rows && d < s.D ? value_at<FQ>(q, d) : 0.f;
-      reinterpret_cast<uint16_t*>(sh + M::kQNew + r * M::kQStride)[d] = (uint16_t)(FQ == KVCRUSH_BF16 ? pack_bf16(v[i], 0.f) : pack_fp16(v[i], 0.f));
-      big = fmaxf(big, fabsf(v[i]));
-      sum += v[i];
+    for (int j = 0; j < 2; ++j) {
+      int pos = t * kTile + j * 8;
+      bool there = true;
+      if constexpr (kPages) {
+        // page = hn / halves_per_page by a product: exact for hn below 2^32 / halves_per_page
+        const int hn = 2 * t + j, page = halves_per_page == 1 ? hn : (int)__umulhi((uint32_t)hn, page_magic);
+        there = page < n_chosen;
+        pos = there ? pages.chosen[page] * a.pages.page_size + (hn - page * halves_per_page) * 8 : 0;
+      }
+      h.n[j] = there ? min(8, max(0, w.seen - pos)) : 0;
+      h.row[j] = w.begin + pos;
     }
+    return h;
+  };
+  auto new_halves = [&](int t) {
+    Halves h;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int first = (t - cached) * kTile + j * 8;
+      h.row[j] = w.first + first;
+      h.n[j] = min(8, max(0, w.own - first));
+    }
+    return h;
+  };
+  // The ring: while a tile is multiplied the next kStages - 1 are under way.  Tiles of new tokens go through it too where they are of
+  // the cache's type.
+  using T = Stage<F, DP>;
+  const uint32_t ring = smem_addr(sh + M::kRing) + warp * M::kRingBytes;
+  const int hi_ring = kScaled ? min(hi, cached) : hi;
+  if (s.D < DP) {                                      // channels that the head does not have are never copied
+    for (int e = lane * 16; e < M::kRingBytes; e += 512)
+      *reinterpret_cast<uint4*>(sh + M::kRing + warp * M::kRingBytes + e) = make_uint4(0u, 0u, 0u, 0u);
+    __syncwarp();
+  }
+  const typename T::Lane of_cache = T::lane_of(src, s.D, lane);
+  auto fetch = [&](int t, int stage) {
+    const uint32_t to = ring + stage * M::kStageBytes;
+    if (t < min(full, hi_ring)) T::template fetch<true>(to, of_cache, halves(t), lane);
+    else if (t < hi_ring) {
+      if constexpr (kScaled) T::template fetch<false>(to, of_cache, halves(t), lane);
+      else if (t < cached) T::template fetch<false>(to, of_cache, halves(t), lane);
+      else T::template fetch<false>(to, T::lane_of(fresh, s.D, lane), new_halves(t), lane);
+    }
+    copies_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < M::kStages - 1; ++i) fetch(lo + warp + i * kWarps, i);
+
+  // queries: a warp takes a row, a lane eight channels
+  for (int r = warp; r < kRows; r += kWarps) {
+    const int d = lane * 8;
+    Raw8<FQ> raw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw.w[i] = 0u;
+    if (r < w.rows && d < s.D)
+      raw.load(static_cast<const unsigned char*>(a.Q.ptr) + bytes_of<FQ>(w.layer * a.Q.sl + (w.first + w.token(s.G, r)) * a.Q.st + (w.hk * s.G + w.head(s.G, r)) * a.Q.sh + d));
+    if (d < DP) *reinterpret_cast<uint4*>(sh + M::kQNew + r * M::kQStride + d * 2) = make_uint4(raw.w[0], raw.w[1], raw.w[2], raw.w[3]);
     if constexpr (kScaled) {
+      float v[8], big = 0.f, sum = 0.f, f = 1.f;
+      raw.widen(v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { big = fmaxf(big, fabsf(v[i])); sum += v[i]; }
+#pragma unroll
+      for (int k = 1; k < 32; k <<= 1) { big = fmaxf(big, __shfl_xor_sync(kAll, big, k)); sum += __shfl_xor_sync(kAll, sum, k); }
       // bf16 queries are multiplied as half precision: a power of two that brings the row's largest value just under 2^15
       // keeps all their bits (those 2^-29 below the largest fade out)
-      float f = 1.f;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) { big = fmaxf(big, __shfl_xor_sync(kAll, big, d)); sum += __shfl_xor_sync(kAll, sum, d); }
       if (FQ == KVCRUSH_BF16 && big > 0.f) {
         const int e = min((int)(__float_as_uint(big) >> 23), 254) - 127;
         f = __uint_as_float((uint32_t)(min(14 - e, 126) + 127) << 23);
       }
 #pragma unroll
-      for (int i = 0; i < DP / 32; ++i) {
-        int d = 32 * i + lane;
-        if (F == KVCRUSH_INT4) d = (d & ~7) | (d & 3) << 1 | (d >> 2 & 1);           // codes of a word pair up as 0 4, 1 5, 2 6, 3 7
-        reinterpret_cast<uint16_t*>(sh + M::kQ + r * M::kQStride)[d] = (uint16_t)pack_fp16(v[i] * f, 0.f);
-      }
+      for (int i = 0; i < 8; ++i) v[i] *= f;
+      // the 4-bit codes of a word pair up as 0 4, 1 5, 2 6, 3 7
+      const uint4 u = F == KVCRUSH_INT4 ? make_uint4(pack_fp16(v[0], v[4]), pack_fp16(v[1], v[5]), pack_fp16(v[2], v[6]), pack_fp16(v[3], v[7]))
+                                        : make_uint4(pack_fp16(v[0], v[1]), pack_fp16(v[2], v[3]), pack_fp16(v[4], v[5]), pack_fp16(v[6], v[7]));
+      if (d < DP) *reinterpret_cast<uint4*>(sh + M::kQ + r * M::kQStride + d * 2) = u;
       if (lane == 0) row_scale[r] = make_float2(a.scale_log2 / f, sum * a.scale_log2);
     }
   }
   __syncthreads();
-  const Queries q{sh + M::kQ, M::kQStride}, q_new{sh + M::kQNew, M::kQStride};
+  const Queries q{smem_addr(sh + M::kQ), M::kQStride}, q_new{smem_addr(sh + M::kQNew), M::kQStride};
   constexpr int kQRegs = kRegs ? NB * DP / 8 : 1;
   uint32_t qr[kQRegs];
   if constexpr (kRegs) {
 #pragma unroll
-    for (int n = 0; n < NB; ++n)
+    for (int n = 0; n < NB; ++n) {
+      if constexpr (!kScaled) {
 #pragma unroll
-      for (int i = 0; i < L::kPieces; ++i)
+        for (int i = 0; i < DP / 32; ++i) {
+          uint32_t v[4];
+          ldmatrix4<false>(v, q.sh + (n * 8 + (lane & 7)) * q.stride + (4 * i + (lane >> 3)) * 16);
 #pragma unroll
-        for (int e = 0; e < L::kChannels / 8; ++e) {
-          const uint4 v = *reinterpret_cast<const uint4*>(q.sh + (n * 8 + g) * q.stride + (L::k_channel(i, c) + 8 * e) * 2);
-          const int at = ((n * L::kPieces + i) * (L::kChannels / 8) + e) * 4;
-          qr[at] = v.x; qr[at + 1] = v.y; qr[at + 2] = v.z; qr[at + 3] = v.w;
+          for (int j = 0; j < 4; ++j) qr[(n * (DP / 32) + i) * 4 + j] = v[j];
         }
+      } else {
+#pragma unroll
+        for (int i = 0; i < L::kPieces; ++i)
+#pragma unroll
+          for (int e = 0; e < L::kChannels / 8; ++e) {
+            uint32_t v[4];
+            shared_words(v, q.sh + (n * 8 + g) * q.stride + (L::k_channel(i, c) + 8 * e) * 2);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) qr[((n * L::kPieces + i) * (L::kChannels / 8) + e) * 4 + j] = v[j];
+          }
+      }
+    }
   }
   float2 rs[NB][2];
   if constexpr (kScaled) {
@@ -512,141 +736,85 @@ attend_kernel(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) run.o[n][t][i] = 0.f;
   }
-
-  const Source src{static_cast<const unsigned char*>(a.K.ptr) + bytes_of<F>(w.layer * a.K.sl + w.hk * a.K.sh),
-                   static_cast<const unsigned char*>(a.V.ptr) + bytes_of<F>(w.layer * a.V.sl + w.hk * a.V.sh),
-                   (uint32_t)bytes_of<F>(a.K.st), (uint32_t)bytes_of<F>(a.V.st), a.K.scales + w.layer * a.K.scl + w.hk * a.K.sch,
-                   a.V.scales + w.layer * a.V.scl + w.hk * a.V.sch, (uint32_t)a.K.sct, (uint32_t)a.V.sct};
-  const int halves_per_page = kPages ? a.pages.page_size / 8 : 1;
-  const int cached = kPages ? (n_chosen * halves_per_page + 1) / 2 : (w.seen + kTile - 1) / kTile;
-  const int n_tiles = cached + (w.own + kTile - 1) / kTile;
-  const int per = (n_tiles + n_blk - 1) / n_blk, lo = min(n_tiles, rank * per), hi = min(n_tiles, lo + per), hi_cached = min(hi, cached);
-  // tiles whose keys all exist and are seen by every query row; of the chosen pages only the last may be short
-  int full;
-  if (kPages) {
-    const int last = n_chosen ? pages.chosen[n_chosen - 1] : 0;
-    full = n_chosen ? ((n_chosen - 1) * a.pages.page_size + min(a.pages.page_size, w.seen - last * a.pages.page_size)) / kTile : 0;
-  } else {
-    full = (w.own ? w.seen : w.limit(s.G, 0)) / kTile;
-  }
-  const int hi_full = min(hi, full);
-  auto halves = [&](int t) {
-    Halves h;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      int pos = t * kTile + j * 8;
-      bool there = true;
-      if constexpr (kPages) {
-        const int hn = 2 * t + j, page = hn / halves_per_page;
-        there = page < n_chosen;
-        pos = there ? pages.chosen[page] * a.pages.page_size + (hn - page * halves_per_page) * 8 : 0;
-      }
-      h.n[j] = there ? min(8, max(0, w.seen - pos)) : 0;
-      h.row[j] = w.begin + pos;
-    }
-    return h;
-  };
-  auto scale_logits = [&](const KeyTile<F, DP>& K, float (&x)[NB][4]) {
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (kScaled) {
-          x[n][i] *= rs[n][i & 1].x * K.sc[i >> 1].x;
-          if (F == KVCRUSH_INT4) x[n][i] = fmaf(fmaf(8.f, K.sc[i >> 1].x, K.sc[i >> 1].y), rs[n][i & 1].y, x[n][i]);
-        } else {
-          x[n][i] *= a.scale_log2;
-        }
-      }
-  };
-  {
-    auto step = [&](const Halves& h, const KeyTile<F, DP>& K, auto&& prefetch) {
-      ValueTile<F, DP> V;
-      V.template load<true>(src, h, s.D, lane);
-      prefetch();
-      float x[NB][4];
-      logits<F, A, DP, NB, kRegs>(K, q, qr, lane, x);
-      scale_logits(K, x);
-      add_tile<F, F, A, DP, NB, kScaled, true>(V, src, h, s.D, x, 0u, false, run, lane);
-    };
-    int t = lo + warp;
-    if constexpr (kAhead) {
-      // while a tile is multiplied the next one's keys are in flight
-      KeyTile<F, DP> k0, k1;
-      Halves h0, h1;
-      if (t < hi_full) { h0 = halves(t); k0.template load<true>(src, h0, s.D, lane); }
-      for (; t < hi_full; t += 2 * kWarps) {
-        step(h0, k0, [&] { if (t + kWarps < hi_full) { h1 = halves(t + kWarps); k1.template load<true>(src, h1, s.D, lane); } });
-        if (t + kWarps >= hi_full) break;
-        step(h1, k1, [&] { if (t + 2 * kWarps < hi_full) { h0 = halves(t + 2 * kWarps); k0.template load<true>(src, h0, s.D, lane); } });
-      }
-    } else {
-      for (; t < hi_full; t += kWarps) {
-        const Halves h = halves(t);
-        KeyTile<F, DP> K;
-        K.template load<true>(src, h, s.D, lane);
-        step(h, K, [] {});
-      }
-    }
-  }
-  // short tiles, and those that some rows see only a part of
-  for (int t = max(lo, full) + warp; t < hi_cached; t += kWarps) {
-    const Halves h = halves(t);
-    KeyTile<F, DP> K;
-    ValueTile<F, DP> V;
-    K.template load<false>(src, h, s.D, lane);
-    V.template load<false>(src, h, s.D, lane);
-    float x[NB][4];
-    logits<F, A, DP, NB, kRegs>(K, q, qr, lane, x);
-    scale_logits(K, x);
+  // keys of the tile that row n * 8 + 2c + (i & 1) does not see
+  auto hide = [&](float (&x)[NB][4], const Halves& h, auto&& sees) {
     uint32_t hidden = 0;
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = n * 8 + 2 * c + (i & 1);
-        if (g >= h.n[i >> 1] || (!kPages && t * kTile + g + (i >> 1) * 8 >= w.limit(s.G, min(r, w.rows - 1)))) {
+      for (int i = 0; i < 4; ++i)
+        if (g >= h.n[i >> 1] || !sees(g + (i >> 1) * 8, min(n * 8 + 2 * c + (i & 1), w.rows - 1))) {
           x[n][i] = neg_inf();
           hidden |= 1u << (4 * n + i);
         }
-      }
-    add_tile<F, F, A, DP, NB, kScaled, false>(V, src, h, s.D, x, hidden, true, run, lane);
-  }
-  // keys among the new tokens
-  if (!kPages && w.own && hi > cached) {
-    const Source fresh{static_cast<const unsigned char*>(a.K_new.ptr) + bytes_of<FQ>(w.layer * a.K_new.sl + w.hk * a.K_new.sh),
-                       static_cast<const unsigned char*>(a.V_new.ptr) + bytes_of<FQ>(w.layer * a.V_new.sl + w.hk * a.V_new.sh),
-                       (uint32_t)bytes_of<FQ>(a.K_new.st), (uint32_t)bytes_of<FQ>(a.V_new.st), nullptr, nullptr, 0, 0};
-    for (int t = max(lo, cached) + warp; t < hi; t += kWarps) {
-      const int first = (t - cached) * kTile;
-      Halves h;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        h.row[j] = w.first + first + j * 8;
-        h.n[j] = min(8, max(0, w.own - first - j * 8));
-      }
-      KeyTile<FQ, DP> K;
-      ValueTile<FQ, DP, F> V;
-      K.template load<false>(fresh, h, s.D, lane);
-      V.template load<false>(fresh, h, s.D, lane);
-      float x[NB][4];
-      const uint32_t none[1] = {0u};
-      logits<FQ, FQ, DP, NB, false>(K, q_new, none, lane, x);
-      uint32_t hidden = 0;
+    return hidden;
+  };
+  int stage = 0;
+  for (int t = lo + warp; t < hi_ring; t += kWarps) {
+    copies_wait<M::kStages - 2>();
+    __syncwarp();
+    fetch(t + (M::kStages - 1) * kWarps, stage == 0 ? M::kStages - 1 : stage - 1);
+    const uint32_t at = ring + stage * M::kStageBytes;
+    float x[NB][4];
+    logits<F, A, DP, NB, kRegs>(at, q, qr, lane, x);
+    if constexpr (kScaled) {
+      const float2 k0 = T::scale(at, false, g), k1 = T::scale(at, false, g + 8);
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int r = min(n * 8 + 2 * c + (i & 1), w.rows - 1), key = g + (i >> 1) * 8;
-          x[n][i] *= a.scale_log2;
-          if (g >= h.n[i >> 1] || !sees_new(a, w, w.token(s.G, r), first + key)) {
-            x[n][i] = neg_inf();
-            hidden |= 1u << (4 * n + i);
-          }
+          const float2 sc = i < 2 ? k0 : k1;
+          x[n][i] *= rs[n][i & 1].x * sc.x;
+          if (F == KVCRUSH_INT4) x[n][i] = fmaf(fmaf(8.f, sc.x, sc.y), rs[n][i & 1].y, x[n][i]);
         }
-      add_tile<FQ, F, FQ, DP, NB, kScaled, false>(V, fresh, h, s.D, x, hidden, true, run, lane);
+    } else {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[n][i] *= a.scale_log2;
+    }
+    uint32_t hidden = 0;
+    Halves h{};
+    if (t >= full) {
+      if (kScaled || t < cached) {
+        h = halves(t);
+        hidden = hide(x, h, [&](int key, int r) { return kPages || t * kTile + key < w.limit(s.G, r); });
+      } else {
+        h = new_halves(t);
+        hidden = hide(x, h, [&](int key, int r) { return sees_new(a, w, w.token(s.G, r), (t - cached) * kTile + key); });
+      }
+    }
+    add_tile<F, F, A, DP, NB>(at, h, s.D, x, hidden, run, lane);
+    stage = stage == M::kStages - 1 ? 0 : stage + 1;
+    __syncwarp();
+  }
+  if constexpr (kScaled && !kPages) {                  // new tokens beside a quantised cache
+    for (int t = max(lo, cached) + warp; t < hi; t += kWarps) {
+      const Halves h = new_halves(t);
+      copies_wait<0>();
+      __syncwarp();
+      using TN = Stage<FQ, DP>;
+      if (s.D < DP) {
+        for (int e = lane * 16; e < TN::kBytes; e += 512) *reinterpret_cast<uint4*>(sh + M::kRing + warp * M::kRingBytes + e) = make_uint4(0u, 0u, 0u, 0u);
+        __syncwarp();
+      }
+      TN::template fetch<false>(ring, TN::lane_of(fresh, s.D, lane), h, lane);
+      copies_commit();
+      copies_wait<0>();
+      __syncwarp();
+      float x[NB][4];
+      const uint32_t none[1] = {0u};
+      logits<FQ, FQ, DP, NB, false>(ring, q_new, none, lane, x);
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[n][i] *= a.scale_log2;
+      const uint32_t hidden = hide(x, h, [&](int key, int r) { return sees_new(a, w, w.token(s.G, r), (t - cached) * kTile + key); });
+      add_tile<FQ, F, FQ, DP, NB>(ring, h, s.D, x, hidden, run, lane);
     }
   }
+  copies_wait<0>();
+  __syncthreads();                                     // the outputs go where the rings were
 
   // the block's warps
   Part* part = reinterpret_cast<Part*>(sh + M::kPart);
@@ -665,8 +833,9 @@ attend_kernel(AttendArgs a) {
 #pragma unroll
       for (int t = 0; t < DP / 16; ++t) {
         float* at = o + (warp * kRows + n * 8 + 2 * c + i) * M::kOStride;
-        // the two channels are neighbours
-        *reinterpret_cast<float2*>(at + L::out_channel(t, g)) = make_float2(run.o[n][t][i], run.o[n][t][i + 2]);
+        const int ch = L::out_channel(t, g);
+        if constexpr (L::kPairStep == 1) *reinterpret_cast<float2*>(at + ch) = make_float2(run.o[n][t][i], run.o[n][t][i + 2]);
+        else { at[ch] = run.o[n][t][i]; at[ch + L::kPairStep] = run.o[n][t][i + 2]; }
       }
     }
   __syncthreads();
@@ -729,8 +898,8 @@ int largest_cluster(Kernel kern, int threads, size_t dyn, std::atomic<int>* know
 
 template <int F, int FQ, int DP, int NB, bool kPages>
 int launch_one(AttendArgs& a, cudaStream_t stream) {
-  // Two blocks an SM at least: a chip has room for 14 clusters of 16 then, with one only for 7.
-  constexpr int kWarps = NB * DP <= 128 ? 8 : 4, kBlocks = NB * DP == 256 ? 3 : 2;
+  // Two blocks an SM: a chip has room for 14 clusters of 16 then, with one only for 7.
+  constexpr int kWarps = NB * DP <= 128 && (kQuantized<F> || DP == 64) ? 8 : 4, kBlocks = Mem<F, FQ, DP, NB, kWarps>::kEnd <= 113 * 1024 ? 2 : 1;
   auto kern = attend_kernel<F, FQ, DP, NB, kWarps, kBlocks, kPages>;
   using M = Mem<F, FQ, DP, NB, kWarps>;
   const Shape& s = a.s;
