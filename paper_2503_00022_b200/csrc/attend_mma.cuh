@@ -43,30 +43,22 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   return d;
 }
 
-__device__ __forceinline__ uint32_t sub_half2(uint32_t a, uint32_t b) {
-  const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&d);
-}
-__device__ __forceinline__ uint32_t fma_half2(uint32_t a, uint32_t b, uint32_t c) {
-  const __half2 d = __hfma2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b), *reinterpret_cast<const __half2*>(&c));
-  return *reinterpret_cast<const uint32_t*>(&d);
-}
 __device__ __forceinline__ uint32_t e4m3_half2(uint32_t two_codes) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two_codes, __NV_E4M3);
   return (uint32_t)h.x | (uint32_t)h.y << 16;
 }
-// Integers as half-precision numbers: the bits of 1024 + n with n in the low mantissa bits, less 1024 and the offset.
-constexpr uint32_t k1024 = 0x64006400u, k1032 = 0x64086408u, k1152 = 0x64806480u, kSixteenth = 0x2C002C00u, kMinus72 = 0xD480D480u;
-// bytes 0 and 1 (hi: 2 and 3) of a word of signed bytes, offset by 128
-template <bool kHi> __device__ __forceinline__ uint32_t int8_half2(uint32_t offset_bytes) {
-  return sub_half2(__byte_perm(offset_bytes, k1024, kHi ? 0x7372 : 0x7170), k1152);
-}
-// the codes (less 8) in bits 4 i of either half word
-template <int I> __device__ __forceinline__ uint32_t int4_half2(uint32_t v) {
-  const uint32_t s = I >= 2 ? v >> 8 : v;
-  if constexpr (I % 2 == 0) return sub_half2((s & 0x000F000Fu) | k1024, k1032);
-  else return fma_half2((s & 0x00F000F0u) | k1024, kSixteenth, kMinus72);
-}
+// Integers as half-precision numbers: a byte or nibble in the low bits of a half word is a subnormal number, n * 2^-24, exactly,
+// and the tensor cores multiply those as they are.  Codes are made unsigned that way: 8-bit ones carry 128 too much, 4-bit ones are
+// taken less 8; what that adds to a sum over channels is known from the queries, and what it adds to a sum over keys from
+// a product with ones.  4-bit codes of odd channels stand four bits higher and count 16 times: their queries are divided by 16,
+// and their outputs.
+constexpr uint32_t kOnes = 0x3C003C00u;
+template <int F> constexpr float kOffset = F == KVCRUSH_INT8 ? 128.f : F == KVCRUSH_INT4 ? 8.f : 0.f;
+template <int F> constexpr bool kInteger = F == KVCRUSH_INT8 || F == KVCRUSH_INT4;
+// bytes 0 and 1 (hi: 2 and 3) of a word
+template <bool kHi> __device__ __forceinline__ uint32_t byte_half2(uint32_t bytes) { return __byte_perm(bytes, 0u, kHi ? 0x4342 : 0x4140); }
+// the codes in bits 4 I of either half word
+template <int I> __device__ __forceinline__ uint32_t int4_half2(uint32_t v) { return (I >= 2 ? v >> 8 : v) & (I % 2 ? 0x00F000F0u : 0x000F000Fu); }
 
 // Where the channels of a head lie in a lane's registers.  DP: channels rounded up to 64, 128 or 256.
 template <int F, int DP>
@@ -108,7 +100,7 @@ template <class T> __device__ __forceinline__ const T* at_row(const T* base, int
 // Operand pairs of a word of a key row: two channels each.
 template <int F>
 __device__ __forceinline__ void key_pairs(uint32_t w, uint32_t (&p)[16 / Bits<F>::value]) {
-  if constexpr (F == KVCRUSH_INT8) { p[0] = int8_half2<false>(w ^ 0x80808080u); p[1] = int8_half2<true>(w ^ 0x80808080u); }
+  if constexpr (F == KVCRUSH_INT8) { p[0] = byte_half2<false>(w ^ 0x80808080u); p[1] = byte_half2<true>(w ^ 0x80808080u); }
   else if constexpr (F == KVCRUSH_E4M3) { p[0] = e4m3_half2(w & 0xFFFFu); p[1] = e4m3_half2(w >> 16); }
   else { p[0] = int4_half2<0>(w); p[1] = int4_half2<1>(w); p[2] = int4_half2<2>(w); p[3] = int4_half2<3>(w); }
 }
@@ -117,7 +109,7 @@ template <int F>
 __device__ __forceinline__ void value_pairs(uint32_t wa, uint32_t wb, uint32_t (&p)[32 / Bits<F>::value]) {
   if constexpr (F == KVCRUSH_INT8) {
     const uint32_t lo = __byte_perm(wa, wb, 0x5140) ^ 0x80808080u, hi = __byte_perm(wa, wb, 0x7362) ^ 0x80808080u;
-    p[0] = int8_half2<false>(lo); p[1] = int8_half2<true>(lo); p[2] = int8_half2<false>(hi); p[3] = int8_half2<true>(hi);
+    p[0] = byte_half2<false>(lo); p[1] = byte_half2<true>(lo); p[2] = byte_half2<false>(hi); p[3] = byte_half2<true>(hi);
   } else if constexpr (F == KVCRUSH_E4M3) {
     const uint32_t lo = __byte_perm(wa, wb, 0x5140), hi = __byte_perm(wa, wb, 0x7362);
     p[0] = e4m3_half2(lo & 0xFFFFu); p[1] = e4m3_half2(lo >> 16); p[2] = e4m3_half2(hi & 0xFFFFu); p[3] = e4m3_half2(hi >> 16);
@@ -235,7 +227,7 @@ struct Stage {
   }
 };
 
-// One channel of row `row` of the values at `tile`; codes without their scale (INT4: less 8).
+// One channel of row `row` of the values at `tile`, of the types that have numbers that are not finite; codes without their scale.
 template <int F, int DP>
 __device__ __forceinline__ float value_at(uint32_t tile, int row, int channel) {
   using T = Stage<F, DP>;
@@ -244,9 +236,7 @@ __device__ __forceinline__ float value_at(uint32_t tile, int row, int channel) {
   shared_words(w, tile + T::at(row, byte >> 4) + (byte & 12));
   if constexpr (F == KVCRUSH_BF16) return (channel & 1) ? unpack_bf16(w[0]).y : unpack_bf16(w[0]).x;
   else if constexpr (F == KVCRUSH_FP16) return (channel & 1) ? unpack_fp16(w[0]).y : unpack_fp16(w[0]).x;
-  else if constexpr (F == KVCRUSH_INT8) return (float)(int)(signed char)(w[0] >> (8 * (channel & 3)));
-  else if constexpr (F == KVCRUSH_E4M3) return unpack_fp16(e4m3_half2(w[0] >> (8 * (channel & 3)) & 0xFFu)).x;
-  else return (float)(int)(w[0] >> (4 * (channel & 7)) & 15u) - 8.f;
+  else return unpack_fp16(e4m3_half2(w[0] >> (8 * (channel & 3)) & 0xFFu)).x;
 }
 // Is any of the four numbers (or two, of 16 bits) of a word not finite?
 template <int F>
@@ -268,11 +258,12 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
 
 // Rows 2c and 2c + 1 of each of NB blocks of eight rows.  m, l: maximum of the logits (log2 domain) and sum of 2^(x - m).
 // m2: what the output is relative to; for a quantised cache the maximum of x + log2(scale of the value row), otherwise m.
-// b: sum of 2^(x - m) * zero of the value row (INT4).
+// b: sum of 2^(x - m) * zero of the value row (INT4).  ones: sum of the rounded weights, as an m-tile of ones gives it (all
+// its rows are alike).
 template <int NB, int DP, bool kScaled>
 struct Running {
   float m[NB][2], l[NB][2], m2[NB][2], b[NB][2];
-  float o[NB][DP / 16][4];
+  float o[NB][DP / 16][4], ones[NB][4];
 };
 
 constexpr float kSlack = 8.f;
@@ -465,6 +456,7 @@ __device__ __forceinline__ void add_tile(uint32_t stage, const Halves& h, int D,
         }
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) { run.o[n][t][i] *= f2; run.o[n][t][i + 2] *= f2; }
+        if (kInteger<FO>) run.ones[n][i] *= f2;
       }
     differences();
   }
@@ -494,7 +486,7 @@ __device__ __forceinline__ void add_tile(uint32_t stage, const Halves& h, int D,
     b0[n] = transpose8x8(A == KVCRUSH_BF16 ? pack_bf16(w[0], w[1]) : pack_fp16(w[0], w[1]));
     b1[n] = transpose8x8(A == KVCRUSH_BF16 ? pack_bf16(w[2], w[3]) : pack_fp16(w[2], w[3]));
   }
-  if (masked) {
+  if (!kInteger<F> && masked) {
     // A weight of 0 takes a value that is not finite along: where there is one, every row adds up the keys that it sees.
     bool bad = false;
     for (uint32_t e = lane * 16; e < (uint32_t)T::kTileBytes; e += 512) {
@@ -536,6 +528,10 @@ __device__ __forceinline__ void add_tile(uint32_t stage, const Halves& h, int D,
 #pragma unroll
     for (int n = 0; n < NB; ++n) mma<A>(run.o[n][t], a0, a1, a2, a3, b0[n], b1[n]);
   };
+  if constexpr (F == FO && kInteger<F>) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) mma<A>(run.ones[n], kOnes, kOnes, kOnes, kOnes, b0[n], b1[n]);
+  }
   if constexpr (F == FO) value_operands<F, DP>(stage, lane, multiply);
   else value_operands_like<F, FO, DP>(stage, lane, multiply);
 }
@@ -677,19 +673,19 @@ attend_kernel(AttendArgs a) {
       for (int i = 0; i < 8; ++i) { big = fmaxf(big, fabsf(v[i])); sum += v[i]; }
 #pragma unroll
       for (int k = 1; k < 32; k <<= 1) { big = fmaxf(big, __shfl_xor_sync(kAll, big, k)); sum += __shfl_xor_sync(kAll, sum, k); }
-      // bf16 queries are multiplied as half precision: a power of two that brings the row's largest value just under 2^15
-      // keeps all their bits (those 2^-29 below the largest fade out)
-      if (FQ == KVCRUSH_BF16 && big > 0.f) {
+      // Queries are multiplied as half precision: a power of two that brings the row's largest value just under 2^15 keeps all
+      // their bits (those 2^-25 below the largest fade out).
+      if (big > 0.f) {
         const int e = min((int)(__float_as_uint(big) >> 23), 254) - 127;
         f = __uint_as_float((uint32_t)(min(14 - e, 126) + 127) << 23);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= f;
+      for (int i = 0; i < 8; ++i) v[i] *= F == KVCRUSH_INT4 && i % 2 ? f * 0.0625f : f;
       // the 4-bit codes of a word pair up as 0 4, 1 5, 2 6, 3 7
       const uint4 u = F == KVCRUSH_INT4 ? make_uint4(pack_fp16(v[0], v[4]), pack_fp16(v[1], v[5]), pack_fp16(v[2], v[6]), pack_fp16(v[3], v[7]))
                                         : make_uint4(pack_fp16(v[0], v[1]), pack_fp16(v[2], v[3]), pack_fp16(v[4], v[5]), pack_fp16(v[6], v[7]));
       if (d < DP) *reinterpret_cast<uint4*>(sh + M::kQ + r * M::kQStride + d * 2) = u;
-      if (lane == 0) row_scale[r] = make_float2(a.scale_log2 / f, sum * a.scale_log2);
+      if (lane == 0) row_scale[r] = make_float2((kInteger<F> ? 0x1p24f : 1.f) * a.scale_log2 / f, sum * a.scale_log2);
     }
   }
   __syncthreads();
@@ -735,6 +731,8 @@ attend_kernel(AttendArgs a) {
     for (int t = 0; t < DP / 16; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) run.o[n][t][i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) run.ones[n][i] = 0.f;
   }
   // keys of the tile that row n * 8 + 2c + (i & 1) does not see
   auto hide = [&](float (&x)[NB][4], const Halves& h, auto&& sees) {
@@ -764,8 +762,8 @@ attend_kernel(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float2 sc = i < 2 ? k0 : k1;
-          x[n][i] *= rs[n][i & 1].x * sc.x;
-          if (F == KVCRUSH_INT4) x[n][i] = fmaf(fmaf(8.f, sc.x, sc.y), rs[n][i & 1].y, x[n][i]);
+          const float f = rs[n][i & 1].x * sc.x;
+          x[n][i] = F == KVCRUSH_E4M3 ? x[n][i] * f : fmaf(x[n][i], f, (F == KVCRUSH_INT8 ? -kOffset<F> * sc.x : sc.y) * rs[n][i & 1].y);
         }
     } else {
 #pragma unroll
@@ -787,6 +785,14 @@ attend_kernel(AttendArgs a) {
     add_tile<F, F, A, DP, NB>(at, h, s.D, x, hidden, run, lane);
     stage = stage == M::kStages - 1 ? 0 : stage + 1;
     __syncwarp();
+  }
+  if constexpr (kInteger<F>) {                         // from units of the integer products to values
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) run.o[n][t][i] = fmaf(run.o[n][t][i], F == KVCRUSH_INT4 && i >= 2 ? 0x1p20f : 0x1p24f, -kOffset<F> * run.ones[n][i & 1]);
   }
   if constexpr (kScaled && !kPages) {                  // new tokens beside a quantised cache
     for (int t = max(lo, cached) + warp; t < hi; t += kWarps) {
