@@ -110,6 +110,7 @@ int make_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* ne
   if (a->O.dtype != a->Q.dtype || a->K.dtype != a->V.dtype || (!K_scales && a->K.dtype != a->Q.dtype)) return KVCRUSH_ERR_INVALID_ARG;
   const int eb = elt_bytes(a->Q.dtype);
   if (a->K.st * eb >= kMaxStep || a->V.st * eb >= kMaxStep || a->K.sct * 4 >= kMaxStep || a->V.sct * 4 >= kMaxStep) return KVCRUSH_ERR_UNSUPPORTED;
+  a->group_magic = s.G > 1 ? 0xFFFFFFFFu / (uint32_t)s.G + 1u : 0u;
   a->row_begin = row_begin_dev;
   a->row_count = row_count_dev;
   a->lse = lse_out_dev;

@@ -5,7 +5,8 @@
 // the new tokens of the sequence times the query heads of the group (with pages: of one new token).  The keys are
 // divided among the blocks, every warp keeps a running maximum, sum and output of its own keys, and the parts are added
 // up through distributed shared memory, so that a call is one launch, needs no scratch memory and gives the same
-// result every time.
+// result every time.  Every block owns a share of the output and is sent the others' parts of it: stores that nobody waits for,
+// one barrier, and what is left is done by each block alone (blocks that read their peers' parts instead took 4 to 7 us).
 #pragma once
 
 #include <cooperative_groups.h>
@@ -27,9 +28,6 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// What exponentials are relative to; without a finite maximum all logits are -inf, which adds 0, or NaN, which stays.
-__device__ __forceinline__ float reference(float maximum) { return maximum == neg_inf() ? 0.f : maximum; }
-
 struct Unit {
   int layer, seq, hk;
   int first;                 // packed index of the first new token of the unit
@@ -38,36 +36,44 @@ struct Unit {
   int begin, seen;           // cached rows: the first one's number, and how many the block's last token sees
   int seen0;                 // how many the unit's token 0 would see (token j: seen0 + j), where own == 0
   int own;                   // keys among the new tokens
-  __device__ __forceinline__ int token(int G, int r) const { return (row0 + r) / G; }
-  __device__ __forceinline__ int head(int G, int r) const { return (row0 + r) % G; }
+  int G;
+  uint32_t magic;
+  __device__ __forceinline__ int token(int r) const { return G == 1 ? row0 + r : (int)__umulhi((uint32_t)(row0 + r), magic); }
+  __device__ __forceinline__ int head(int r) const { return row0 + r - token(r) * G; }
   // cached rows that the token of row r sees
-  __device__ __forceinline__ int limit(int G, int r) const { return own ? seen : min(max(seen0 + token(G, r), 0), seen); }
+  __device__ __forceinline__ int limit(int r) const { return own ? seen : min(max(seen0 + token(r), 0), seen); }
 };
 
-// Unit number u; false: no rows (uniform over the cluster).
+// The unit of this block's cluster; false: no rows (uniform over the cluster).  Grid: (clusters of a layer and sequence, or of a
+// layer and new token; KV heads; blocks of query rows).
 template <bool kPages>
-__device__ __forceinline__ bool unit_of(const AttendArgs& a, unsigned u, int rows_per_block, Unit& w) {
+__device__ __forceinline__ bool unit_of(const AttendArgs& a, int rows_per_block, Unit& w) {
   const Shape& s = a.s;
-  const int rb = (int)(u % a.row_blocks); u /= a.row_blocks;
-  w.hk = (int)(u % s.Hkv); u /= s.Hkv;
-  int count, j_last;
+  unsigned u;
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(u));
+  w.hk = blockIdx.y;
+  w.row0 = (int)blockIdx.z * rows_per_block;
+  w.G = s.G; w.magic = a.group_magic;
+  const unsigned per_layer = kPages ? a.fresh.total : s.n_seqs;
+  w.layer = u < per_layer ? 0 : (int)(u / per_layer);
+  u -= w.layer * per_layer;
+  int count;
   if (kPages) {
-    w.first = (int)(u % a.fresh.total); w.layer = (int)(u / a.fresh.total);
+    w.first = (int)u;
     w.seq = seq_of_token(a.fresh.cu, s.n_seqs, w.first);
     rows_of(s, a.row_begin, a.row_count, w.layer, w.seq, w.begin, count);
     w.seen0 = count - (__ldg(a.fresh.cu + w.seq + 1) - 1 - w.first);
     w.n_tok = 1;
   } else {
-    w.seq = (int)(u % s.n_seqs); w.layer = (int)(u / s.n_seqs);
+    w.seq = (int)u;
     w.first = __ldg(a.fresh.cu + w.seq);
     w.n_tok = __ldg(a.fresh.cu + w.seq + 1) - w.first;
     rows_of(s, a.row_begin, a.row_count, w.layer, w.seq, w.begin, count);
     w.seen0 = count - w.n_tok + 1;
   }
-  w.row0 = rb * rows_per_block;
   w.rows = min(rows_per_block, w.n_tok * s.G - w.row0);
   if (w.rows <= 0) return false;
-  j_last = (w.row0 + w.rows - 1) / s.G;
+  const int j_last = w.token(w.rows - 1);
   if (!kPages && a.K_new.ptr) {
     w.seen = count;
     w.own = a.fresh.mask ? w.n_tok : j_last + 1;
@@ -249,68 +255,124 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
 
 // ---- the sum over the cluster -----------------------------------------------------------------------------
 
-// A block's part of a row: maximum and sum of the weights, what its output is relative to, and the sum of weights times zeros.
+// A part of a row: maximum and sum of the weights, what its output is relative to, and the sum of weights times zeros.
 struct Part { float m, l, m2, b; };
 
-// Adds up the blocks' parts and writes the unit's rows; all threads of the cluster.  o: [rows][stride] this block's output,
-// part: [rows], factor: [rows][kMaxCluster + 1] scratch, all in shared memory at the same place in every block.
-template <int FQ, int kThreads>
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Where a block receives the parts of its share of the output: four channels of a row make an element.
+template <int kRows, int kMaxD>
+struct Received {
+  float4 o[kRows * kMaxD / 4 + kMaxCluster];           // [block][element of the share]
+  Part part[kMaxCluster * kRows];                      // [block][row]
+};
+
+// Adds up the warps' parts, then the blocks', and writes the unit's rows; all threads of the cluster.  o: [kWarps][kRows][stride]
+// outputs, part: [kWarps][kRows], both of this block.  The caller has arrived at the cluster's barrier once (so that the
+// peers are known to run) and not waited.
+template <int FQ, int kWarps, int kRows, int kMaxD>
 __device__ __forceinline__ void join_and_write(const AttendArgs& a, const Unit& w, cg::cluster_group& cluster, int n_blk, int rank,
-                                               float* o, int stride, Part* part, float* factor) {
+                                               const float* o, int stride, const Part* part, Received<kRows, kMaxD>* recv) {
   using namespace fmt;
+  constexpr int kThreads = kWarps * 32;
   const Shape& s = a.s;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (n_blk > 1) cluster.sync(); else __syncthreads();
-  for (int r = warp; r < w.rows; r += kThreads / 32) {
-    Part p{neg_inf(), 0.f, neg_inf(), 0.f};
-    if (lane < n_blk) p = n_blk > 1 ? *cluster.map_shared_rank(part + r, lane) : part[r];
-    float M = p.m;
-#pragma unroll
-    for (int d = 1; d < kMaxCluster; d <<= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, d));
-    const float ref = reference(M), f = exp2f(p.m - ref);
-    float l = p.l == 0.f ? 0.f : p.l * f, b = p.l == 0.f ? 0.f : p.b * f;
-#pragma unroll
-    for (int d = 1; d < kMaxCluster; d <<= 1) { l += __shfl_xor_sync(kAll, l, d); b += __shfl_xor_sync(kAll, b, d); }
-    if (lane < n_blk) factor[r * (kMaxCluster + 1) + lane] = l == 0.f ? 0.f : exp2f(p.m2 - ref) / l;
-    if (lane == 0) {
-      factor[r * (kMaxCluster + 1) + kMaxCluster] = l == 0.f ? 0.f : b / l;
-      if (rank == 0 && a.lse)
-        a.lse[((long long)w.layer * s.Hq + w.hk * s.G + w.head(s.G, r)) * a.fresh.total + w.first + w.token(s.G, r)] =
-            l == 0.f ? neg_inf() : (M + log2f(l)) * 0.6931471805599453f;
-    }
-  }
+  const int tid = threadIdx.x;
+  const int vec = s.D / 4, total = w.rows * vec;
+  const int per = n_blk == 1 ? total : (total + n_blk - 1) / n_blk;
+  const uint32_t per_magic = 0xFFFFFFFFu / (uint32_t)per + 1u;                    // e / per for e < 2^16 (per > 1)
+  if (n_blk > 1) cluster_wait();
   __syncthreads();
-  // this block's share of the elements, eight channels a thread
-  const int vec = s.D / 8, total = w.rows * vec, per = (total + n_blk - 1) / n_blk;
-  for (int e = rank * per + tid; e < min(total, (rank + 1) * per); e += kThreads) {
-    const int r = e / vec, c = (e - r * vec) * 8;
-    const float* f = factor + r * (kMaxCluster + 1);
-    float x[8];
+  for (int r = tid; r < w.rows * n_blk; r += kThreads) {                         // a row's part, to every block
+    const int row = r % w.rows, to = r / w.rows;
+    float m = -FLT_MAX, m2 = -FLT_MAX, l = 0.f, b = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = f[kMaxCluster];
-    for (int b = 0; b < n_blk; ++b) {
-      const float* peer = n_blk > 1 ? cluster.map_shared_rank(o, b) : o;
-      const float fb = f[b];
-      const float4 u = *reinterpret_cast<const float4*>(peer + r * stride + c), v = *reinterpret_cast<const float4*>(peer + r * stride + c + 4);
-      x[0] = fmaf(u.x, fb, x[0]); x[1] = fmaf(u.y, fb, x[1]); x[2] = fmaf(u.z, fb, x[2]); x[3] = fmaf(u.w, fb, x[3]);
-      x[4] = fmaf(v.x, fb, x[4]); x[5] = fmaf(v.y, fb, x[5]); x[6] = fmaf(v.z, fb, x[6]); x[7] = fmaf(v.w, fb, x[7]);
+    for (int k = 0; k < kWarps; ++k) { m = fmaxf(m, part[k * kRows + row].m); m2 = fmaxf(m2, part[k * kRows + row].m2); }
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) {
+      const Part p = part[k * kRows + row];
+      const float f = ex2(p.m - m);
+      l = fmaf(p.l, f, l);
+      b = fmaf(p.b, f, b);
     }
-    Raw8<FQ> out;
-    out.narrow(x);
-    unsigned char* op = static_cast<unsigned char*>(const_cast<void*>(a.O.ptr)) +
-        bytes_of<FQ>(w.layer * a.O.sl + (w.first + w.token(s.G, r)) * a.O.st + (w.hk * s.G + w.head(s.G, r)) * a.O.sh + c);
-    out.store(op);
+    Part* dst = recv->part + rank * kRows + row;
+    *(n_blk > 1 ? cluster.map_shared_rank(dst, to) : dst) = Part{m, l, m2, b};
   }
-  if (n_blk > 1) cluster.sync();             // peers may still read this block's part
+  for (int e = tid; e < total; e += kThreads) {                                 // an element, to its owner
+    const int row = e / vec, d = (e - row * vec) * 4;
+    float m2 = -FLT_MAX;
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) m2 = fmaxf(m2, part[k * kRows + row].m2);
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) {
+      const float f = ex2(part[k * kRows + row].m2 - m2);
+      const float4 v = *reinterpret_cast<const float4*>(o + (k * kRows + row) * stride + d);
+      sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
+    }
+    const int owner = per == 1 ? e : (int)__umulhi((uint32_t)e, per_magic);
+    float4* dst = recv->o + rank * per + (n_blk == 1 ? e : e - owner * per);
+    *(n_blk > 1 ? cluster.map_shared_rank(dst, owner) : dst) = sum;
+  }
+  if (n_blk > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+  const int mine = rank * per;
+  for (int i = tid; i < min(per, total - mine); i += kThreads) {
+    const int e = mine + i, row = e / vec, d = (e - row * vec) * 4;
+    float M = neg_inf();
+    for (int p = 0; p < n_blk; ++p) M = fmaxf(M, recv->part[p * kRows + row].m);
+    float l = 0.f, b = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < n_blk; ++p) {
+      const Part q = recv->part[p * kRows + row];
+      const float4 v = recv->o[p * per + i];
+      const float f = ex2(q.m - M), f2 = ex2(q.m2 - M);
+      l = fmaf(q.l, f, l);
+      b = fmaf(q.b, f, b);
+      // a block without weights has no output either, whatever its maximum
+      sum.x += v.x == 0.f ? 0.f : v.x * f2; sum.y += v.y == 0.f ? 0.f : v.y * f2;
+      sum.z += v.z == 0.f ? 0.f : v.z * f2; sum.w += v.w == 0.f ? 0.f : v.w * f2;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float x[4] = {(sum.x + b) * inv, (sum.y + b) * inv, (sum.z + b) * inv, (sum.w + b) * inv};
+    const int token = w.token(row), head = w.hk * w.G + row + w.row0 - token * w.G;
+    unsigned char* op = static_cast<unsigned char*>(const_cast<void*>(a.O.ptr)) +
+        bytes_of<FQ>(w.layer * a.O.sl + (w.first + token) * a.O.st + head * a.O.sh + d);
+    if constexpr (FQ == KVCRUSH_FP32) *reinterpret_cast<float4*>(op) = make_float4(x[0], x[1], x[2], x[3]);
+    else if constexpr (FQ == KVCRUSH_BF16) *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+    else *reinterpret_cast<uint2*>(op) = make_uint2(pack_fp16(x[0], x[1]), pack_fp16(x[2], x[3]));
+    if (d == 0 && a.lse)
+      a.lse[((long long)w.layer * s.Hq + head) * a.fresh.total + w.first + token] = l == 0.f ? neg_inf() : (M + log2f(l)) * 0.6931471805599453f;
+  }
 }
 
 // ---- host: the launch ------------------------------------------------------------------------------------------
 
-// Blocks of a cluster: enough of them to fill the chip, none with fewer than a tile for each of its warps.
+// Blocks of a cluster: about one round of the blocks that the chip holds (what a block does once, some microseconds, costs as much
+// as a few hundred keys), none with fewer than a tile for each of its warps.
 inline int cluster_size(long long units, int tiles, int warps, int largest, int blocks_wanted) {
   int n = 1;
-  while (n < largest && units * n < blocks_wanted && tiles > n * warps) n *= 2;
+  while (n < largest && 2 * units * n <= blocks_wanted && tiles > n * warps) n *= 2;
   return n;
+}
+// The grid of clusters of n_blk blocks; false: too large.
+inline bool attend_grid(const AttendArgs& a, int rows_per_block, int n_blk, dim3* grid) {
+  const bool pages = a.pages.page_size > 0;
+  const long long rows = (long long)(pages ? 1 : a.fresh.most) * a.s.G, x = (long long)a.s.n_layers * (pages ? a.fresh.total : a.s.n_seqs) * n_blk;
+  *grid = dim3((unsigned)x, (unsigned)a.s.Hkv, (unsigned)((rows + rows_per_block - 1) / rows_per_block));
+  return x <= 0x7FFFFFFFLL && grid->z <= 65535u;
+}
+inline long long attend_units(const AttendArgs& a, int rows_per_block) {
+  dim3 g;
+  attend_grid(a, rows_per_block, 1, &g);
+  return (long long)a.s.n_layers * (a.pages.page_size > 0 ? a.fresh.total : a.s.n_seqs) * g.y * g.z;
+}
+inline int attend_tiles(const AttendArgs& a) {
+  const PageChoice& p = a.pages;
+  const long long keys = p.page_size > 0 ? (long long)(p.budget < p.max_pages ? p.budget : p.max_pages) * p.page_size
+                                         : (long long)a.s.max_seqlen + (a.K_new.ptr ? a.fresh.most : 0);
+  return (int)((keys + kTile - 1) / kTile);
 }
 
 }  // namespace att

@@ -546,13 +546,14 @@ struct Mem {
   static constexpr int kQ = 0;                                                    // queries in the cache's order
   static constexpr int kQNew = kQuantized<F> ? kQ + kRows * kQStride : kQ;        // queries as they are
   static constexpr int kRowScale = kQNew + kRows * kQStride;                      // [kRows] factor and sum of the queries
-  static constexpr int kPart = kRowScale + kRows * 8;                             // [kWarps + 1][kRows] Part
-  static constexpr int kFactor = kPart + (kWarps + 1) * kRows * (int)sizeof(Part);
-  static constexpr int kRing = (kFactor + kRows * (kMaxCluster + 1) * 4 + 127) / 128 * 128;
+  static constexpr int kPart = kRowScale + kRows * 8;                             // [kWarps][kRows] Part
+  static constexpr int kRecv = kPart + kWarps * kRows * (int)sizeof(Part);
+  static constexpr int kRing = (kRecv + (int)sizeof(Received<kRows, DP>) + 127) / 128 * 128;
   static constexpr int kO = kRing;
-  // 96 KB of rings a block: as many stages as fit, two at least, and room for a tile of 16-bit new tokens
+  // At most 96 KB of rings a block, less where two blocks would not fit an SM: as many stages as that holds, two at least, and
+  // room for a tile of 16-bit new tokens.
   static constexpr int kStageBytes = (Stage<F, DP>::kBytes + 127) / 128 * 128;
-  static constexpr int kWarpBytes = 96 * 1024 / kWarps;
+  static constexpr int kWarpBytes = (kRing > 16 * 1024 ? 112 * 1024 - kRing : 96 * 1024) / kWarps;
   static constexpr int kStages = kWarpBytes / kStageBytes < 2 ? 2 : kWarpBytes / kStageBytes > 6 ? 6 : kWarpBytes / kStageBytes;
   static constexpr int kNewBytes = kQuantized<F> ? Stage<FQ, DP>::kBytes : 0;
   static constexpr int kRingBytes = kStages * kStageBytes > kNewBytes ? kStages * kStageBytes : kNewBytes;
@@ -576,13 +577,14 @@ attend_kernel(AttendArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   const Shape& s = a.s;
   Unit w;
-  if (!unit_of<kPages>(a, blockIdx.x / n_blk, kRows, w)) return;
+  if (!unit_of<kPages>(a, kRows, w)) return;
   PageMem pages{};
   int n_chosen = 0;
   if constexpr (kPages) {
     pages = page_mem(sh + (M::kEnd + 15) / 16 * 16, a.pages.max_pages, a.pages.budget, s.D);
     n_chosen = choose_pages<FQ, kWarps * 32>(a, w, cluster, n_blk, rank, pages);
   }
+  if (n_blk > 1) cluster_arrive_relaxed();
   float2* row_scale = reinterpret_cast<float2*>(sh + M::kRowScale);
   const Source src{static_cast<const unsigned char*>(a.K.ptr) + bytes_of<F>(w.layer * a.K.sl + w.hk * a.K.sh),
                    static_cast<const unsigned char*>(a.V.ptr) + bytes_of<F>(w.layer * a.V.sl + w.hk * a.V.sh),
@@ -604,7 +606,7 @@ attend_kernel(AttendArgs a) {
     const int last = n_chosen ? pages.chosen[n_chosen - 1] : 0;
     full = n_chosen ? ((n_chosen - 1) * a.pages.page_size + min(a.pages.page_size, w.seen - last * a.pages.page_size)) / kTile : 0;
   } else {
-    full = (w.own ? w.seen : w.limit(s.G, 0)) / kTile;
+    full = (w.own ? w.seen : w.limit(0)) / kTile;
   }
   auto halves = [&](int t) {
     Halves h;
@@ -657,35 +659,44 @@ attend_kernel(AttendArgs a) {
 #pragma unroll
   for (int i = 0; i < M::kStages - 1; ++i) fetch(lo + warp + i * kWarps, i);
 
-  // queries: a warp takes a row, a lane eight channels
-  for (int r = warp; r < kRows; r += kWarps) {
-    const int d = lane * 8;
-    Raw8<FQ> raw;
+  // queries: DP / 8 lanes take a row, a lane eight channels; all rows are loaded before the first is used
+  {
+    constexpr int kLanes = DP / 8, kPerStep = kWarps * 32 / kLanes, kQSteps = (kRows + kPerStep - 1) / kPerStep;
+    const int d = (tid % kLanes) * 8, r0 = tid / kLanes;
+    Raw8<FQ> raw[kQSteps];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) raw.w[i] = 0u;
-    if (r < w.rows && d < s.D)
-      raw.load(static_cast<const unsigned char*>(a.Q.ptr) + bytes_of<FQ>(w.layer * a.Q.sl + (w.first + w.token(s.G, r)) * a.Q.st + (w.hk * s.G + w.head(s.G, r)) * a.Q.sh + d));
-    if (d < DP) *reinterpret_cast<uint4*>(sh + M::kQNew + r * M::kQStride + d * 2) = make_uint4(raw.w[0], raw.w[1], raw.w[2], raw.w[3]);
-    if constexpr (kScaled) {
-      float v[8], big = 0.f, sum = 0.f, f = 1.f;
-      raw.widen(v);
+    for (int u = 0; u < kQSteps; ++u) {
+      const int r = r0 + u * kPerStep;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { big = fmaxf(big, fabsf(v[i])); sum += v[i]; }
+      for (int i = 0; i < 4; ++i) raw[u].w[i] = 0u;
+      if (r < w.rows && d < s.D)
+        raw[u].load(static_cast<const unsigned char*>(a.Q.ptr) + bytes_of<FQ>(w.layer * a.Q.sl + (w.first + w.token(r)) * a.Q.st + (w.hk * s.G + w.head(r)) * a.Q.sh + d));
+    }
 #pragma unroll
-      for (int k = 1; k < 32; k <<= 1) { big = fmaxf(big, __shfl_xor_sync(kAll, big, k)); sum += __shfl_xor_sync(kAll, sum, k); }
-      // Queries are multiplied as half precision: a power of two that brings the row's largest value just under 2^15 keeps all
-      // their bits (those 2^-25 below the largest fade out).
-      if (big > 0.f) {
-        const int e = min((int)(__float_as_uint(big) >> 23), 254) - 127;
-        f = __uint_as_float((uint32_t)(min(14 - e, 126) + 127) << 23);
+    for (int u = 0; u < kQSteps; ++u) {
+      const int r = r0 + u * kPerStep;
+      if (r < kRows) *reinterpret_cast<uint4*>(sh + M::kQNew + r * M::kQStride + d * 2) = make_uint4(raw[u].w[0], raw[u].w[1], raw[u].w[2], raw[u].w[3]);
+      if constexpr (kScaled) {
+        float v[8], big = 0.f, sum = 0.f, f = 1.f;
+        raw[u].widen(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { big = fmaxf(big, fabsf(v[i])); sum += v[i]; }
+#pragma unroll
+        for (int k = 1; k < kLanes; k <<= 1) { big = fmaxf(big, __shfl_xor_sync(kAll, big, k)); sum += __shfl_xor_sync(kAll, sum, k); }
+        // Queries are multiplied as half precision: a power of two that brings the row's largest value just under 2^15 keeps all
+        // their bits (those 2^-25 below the largest fade out).
+        if (big > 0.f) {
+          const int e = min((int)(__float_as_uint(big) >> 23), 254) - 127;
+          f = __uint_as_float((uint32_t)(min(14 - e, 126) + 127) << 23);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= F == KVCRUSH_INT4 && i % 2 ? f * 0.0625f : f;
+        // the 4-bit codes of a word pair up as 0 4, 1 5, 2 6, 3 7
+        const uint4 x = F == KVCRUSH_INT4 ? make_uint4(pack_fp16(v[0], v[4]), pack_fp16(v[1], v[5]), pack_fp16(v[2], v[6]), pack_fp16(v[3], v[7]))
+                                          : make_uint4(pack_fp16(v[0], v[1]), pack_fp16(v[2], v[3]), pack_fp16(v[4], v[5]), pack_fp16(v[6], v[7]));
+        if (r < kRows) *reinterpret_cast<uint4*>(sh + M::kQ + r * M::kQStride + d * 2) = x;
+        if (r < kRows && d == 0) row_scale[r] = make_float2((kInteger<F> ? 0x1p24f : 1.f) * a.scale_log2 / f, sum * a.scale_log2);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= F == KVCRUSH_INT4 && i % 2 ? f * 0.0625f : f;
-      // the 4-bit codes of a word pair up as 0 4, 1 5, 2 6, 3 7
-      const uint4 u = F == KVCRUSH_INT4 ? make_uint4(pack_fp16(v[0], v[4]), pack_fp16(v[1], v[5]), pack_fp16(v[2], v[6]), pack_fp16(v[3], v[7]))
-                                        : make_uint4(pack_fp16(v[0], v[1]), pack_fp16(v[2], v[3]), pack_fp16(v[4], v[5]), pack_fp16(v[6], v[7]));
-      if (d < DP) *reinterpret_cast<uint4*>(sh + M::kQ + r * M::kQStride + d * 2) = u;
-      if (lane == 0) row_scale[r] = make_float2((kInteger<F> ? 0x1p24f : 1.f) * a.scale_log2 / f, sum * a.scale_log2);
     }
   }
   __syncthreads();
@@ -776,10 +787,10 @@ attend_kernel(AttendArgs a) {
     if (t >= full) {
       if (kScaled || t < cached) {
         h = halves(t);
-        hidden = hide(x, h, [&](int key, int r) { return kPages || t * kTile + key < w.limit(s.G, r); });
+        hidden = hide(x, h, [&](int key, int r) { return kPages || t * kTile + key < w.limit(r); });
       } else {
         h = new_halves(t);
-        hidden = hide(x, h, [&](int key, int r) { return sees_new(a, w, w.token(s.G, r), (t - cached) * kTile + key); });
+        hidden = hide(x, h, [&](int key, int r) { return sees_new(a, w, w.token(r), (t - cached) * kTile + key); });
       }
     }
     add_tile<F, F, A, DP, NB>(at, h, s.D, x, hidden, run, lane);
@@ -815,7 +826,7 @@ attend_kernel(AttendArgs a) {
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[n][i] *= a.scale_log2;
-      const uint32_t hidden = hide(x, h, [&](int key, int r) { return sees_new(a, w, w.token(s.G, r), (t - cached) * kTile + key); });
+      const uint32_t hidden = hide(x, h, [&](int key, int r) { return sees_new(a, w, w.token(r), (t - cached) * kTile + key); });
       add_tile<FQ, F, FQ, DP, NB>(ring, h, s.D, x, hidden, run, lane);
     }
   }
@@ -824,7 +835,6 @@ attend_kernel(AttendArgs a) {
 
   // the block's warps
   Part* part = reinterpret_cast<Part*>(sh + M::kPart);
-  Part* warp_part = part + kRows;
   float* o = reinterpret_cast<float*>(sh + M::kO);
 #pragma unroll
   for (int n = 0; n < NB; ++n)
@@ -835,7 +845,7 @@ attend_kernel(AttendArgs a) {
         run.l[n][i] += __shfl_xor_sync(kAll, run.l[n][i], d);
         if (F == KVCRUSH_INT4) run.b[n][i] += __shfl_xor_sync(kAll, run.b[n][i], d);
       }
-      if (g == 0) warp_part[warp * kRows + n * 8 + 2 * c + i] = Part{run.m[n][i], run.l[n][i], kScaled ? run.m2[n][i] : run.m[n][i], run.b[n][i]};
+      if (g == 0) part[warp * kRows + n * 8 + 2 * c + i] = Part{run.m[n][i], run.l[n][i], kScaled ? run.m2[n][i] : run.m[n][i], run.b[n][i]};
 #pragma unroll
       for (int t = 0; t < DP / 16; ++t) {
         float* at = o + (warp * kRows + n * 8 + 2 * c + i) * M::kOStride;
@@ -844,32 +854,7 @@ attend_kernel(AttendArgs a) {
         else { at[ch] = run.o[n][t][i]; at[ch + L::kPairStep] = run.o[n][t][i + 2]; }
       }
     }
-  __syncthreads();
-  if (tid < kRows) {
-    float m = -FLT_MAX, l = 0.f, m2 = -FLT_MAX, b = 0.f;
-    for (int k = 0; k < kWarps; ++k) { m = fmaxf(m, warp_part[k * kRows + tid].m); m2 = fmaxf(m2, warp_part[k * kRows + tid].m2); }
-    for (int k = 0; k < kWarps; ++k) {
-      Part& p = warp_part[k * kRows + tid];
-      const float f = ex2(p.m - m);
-      l = fmaf(p.l, f, l);
-      b = fmaf(p.b, f, b);
-      p.b = ex2(p.m2 - m2);                              // factor of the warp's output
-    }
-    part[tid] = Part{m, l, m2, b};
-  }
-  __syncthreads();
-  for (int e = tid; e < w.rows * (DP / 4); e += kWarps * 32) {
-    const int r = e / (DP / 4), d = (e - r * (DP / 4)) * 4;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) {
-      const float f = warp_part[k * kRows + r].b;
-      const float4 v = *reinterpret_cast<const float4*>(o + (k * kRows + r) * M::kOStride + d);
-      sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
-    }
-    *reinterpret_cast<float4*>(o + r * M::kOStride + d) = sum;
-  }
-  join_and_write<FQ, kWarps * 32>(a, w, cluster, n_blk, rank, o, M::kOStride, part, reinterpret_cast<float*>(sh + M::kFactor));
+  join_and_write<FQ, kWarps, kRows, DP>(a, w, cluster, n_blk, rank, o, M::kOStride, part, reinterpret_cast<Received<kRows, DP>*>(sh + M::kRecv));
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------
@@ -909,19 +894,15 @@ int launch_one(AttendArgs& a, cudaStream_t stream) {
   auto kern = attend_kernel<F, FQ, DP, NB, kWarps, kBlocks, kPages>;
   using M = Mem<F, FQ, DP, NB, kWarps>;
   const Shape& s = a.s;
-  const long long rows = (long long)(kPages ? 1 : a.fresh.most) * s.G;
-  a.row_blocks = (int)((rows + M::kRows - 1) / M::kRows);
-  const long long units = (long long)s.n_layers * (kPages ? a.fresh.total : s.n_seqs) * s.Hkv * a.row_blocks;
-  const long long keys = kPages ? (long long)(a.pages.budget < a.pages.max_pages ? a.pages.budget : a.pages.max_pages) * a.pages.page_size
-                                : (long long)s.max_seqlen + (a.K_new.ptr ? a.fresh.most : 0);
   constexpr int most = (M::kEnd + 15) / 16 * 16;
   const size_t dyn = most + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
   constexpr int bound = most + (kPages ? kMaxPagesPerSeq * 12 + 256 * 16 + 2048 : 0);
   if (allow_dynamic_smem(kern, bound) != KVCRUSH_OK) return KVCRUSH_ERR_CUDA;
   static std::atomic<int> known[kMaxDevices];
-  const int n_blk = cluster_size(units, (int)((keys + kTile - 1) / kTile), kWarps, largest_cluster(kern, kWarps * 32, bound, known), 4 * sm_count());
-  if (units * n_blk > 0x7FFFFFFFLL) return KVCRUSH_ERR_UNSUPPORTED;
-  return launch_chained(kern, dim3((unsigned)(units * n_blk)), dim3(kWarps * 32), dyn, stream, n_blk, a);
+  const int n_blk = cluster_size(attend_units(a, M::kRows), attend_tiles(a), kWarps, largest_cluster(kern, kWarps * 32, bound, known), 2 * sm_count());
+  dim3 grid;
+  if (!attend_grid(a, M::kRows, n_blk, &grid)) return KVCRUSH_ERR_UNSUPPORTED;
+  return launch_chained(kern, grid, dim3(kWarps * 32), dyn, stream, n_blk, a);
 }
 
 // Query rows of a block: as many as there are, up to 32 (16 with more than 128 channels, whose output takes the registers).

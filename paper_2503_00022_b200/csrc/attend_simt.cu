@@ -14,6 +14,7 @@ using namespace fmt;
 constexpr int kWarps = 4;
 constexpr int kRows = 8;                     // query rows of a unit
 constexpr int kMaxD = 256;
+constexpr int kOBytes = kWarps * kRows * kMaxD * 4;
 
 // Four consecutive channels: values, or codes.
 template <int F>
@@ -95,11 +96,11 @@ __device__ __forceinline__ void tile(const CacheView& K, const CacheView& V, lon
     float big = fmaxf(x[i], x[i + 2]);
 #pragma unroll
     for (int d = 4; d < 32; d <<= 1) big = fmaxf(big, __shfl_xor_sync(kAll, big, d));
-    const float m = fmaxf(run.m[i], big), ref = reference(m);
-    corr[i] = exp2f(run.m[i] - ref);
+    const float m = fmaxf(run.m[i], big);                // from the lowest finite number on: logits of -inf have weight 0
+    corr[i] = ex2(run.m[i] - m);
     run.m[i] = m;
-    x[i] = seen[i] ? exp2f(x[i] - ref) : -1.f;
-    x[i + 2] = seen[i + 2] ? exp2f(x[i + 2] - ref) : -1.f;
+    x[i] = seen[i] ? ex2(x[i] - m) : -1.f;
+    x[i + 2] = seen[i + 2] ? ex2(x[i + 2] - m) : -1.f;
     run.l[i] = run.l[i] * corr[i] + (seen[i] ? x[i] : 0.f) + (seen[i + 2] ? x[i + 2] : 0.f);
   }
   __syncwarp();
@@ -153,12 +154,11 @@ __device__ __forceinline__ void tile(const CacheView& K, const CacheView& V, lon
 template <int FQ, int F, bool kPages>
 __global__ void __launch_bounds__(kWarps * 32)
 attend_simt_kernel(AttendArgs a) {
-  extern __shared__ __align__(16) unsigned char page_sh[];
+  extern __shared__ __align__(16) unsigned char dyn_sh[];            // outputs of the warps, then what the choice of pages needs
   __shared__ __align__(16) float q_sh[kRows * kMaxD];
   __shared__ __align__(16) float p_all[kWarps][kTile * kRows];
-  __shared__ __align__(16) float o_sh[kRows * kMaxD];
-  __shared__ Part warp_part[kWarps][kRows], part[kRows];
-  __shared__ float factor[kRows * (kMaxCluster + 1)];
+  __shared__ Part warp_part[kWarps][kRows];
+  __shared__ __align__(16) Received<kRows, kMaxD> recv;
   chain_wait();
   chain_trigger();
   cg::cluster_group cluster = cg::this_cluster();
@@ -166,22 +166,23 @@ attend_simt_kernel(AttendArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   const Shape& s = a.s;
   Unit w;
-  if (!unit_of<kPages>(a, blockIdx.x / n_blk, kRows, w)) return;
+  if (!unit_of<kPages>(a, kRows, w)) return;
   PageMem pages{};
   int n_chosen = 0;
   if constexpr (kPages) {
-    pages = page_mem(page_sh, a.pages.max_pages, a.pages.budget, s.D);
+    pages = page_mem(dyn_sh + kOBytes, a.pages.max_pages, a.pages.budget, s.D);
     n_chosen = choose_pages<FQ, kWarps * 32>(a, w, cluster, n_blk, rank, pages);
   }
+  if (n_blk > 1) cluster_arrive_relaxed();
   for (int e = tid; e < kRows * s.D; e += kWarps * 32) {
     const int r = e / s.D, d = e - r * s.D;
-    q_sh[r * kMaxD + d] = r < w.rows ? (float)widen1<FQ>(a.Q.ptr, w.layer * a.Q.sl + (w.first + w.token(s.G, r)) * a.Q.st +
-                                                                     (w.hk * s.G + w.head(s.G, r)) * a.Q.sh + d) : 0.f;
+    q_sh[r * kMaxD + d] = r < w.rows ? (float)widen1<FQ>(a.Q.ptr, w.layer * a.Q.sl + (w.first + w.token(r)) * a.Q.st +
+                                                                     (w.hk * s.G + w.head(r)) * a.Q.sh + d) : 0.f;
   }
   __syncthreads();
   Running run;
 #pragma unroll
-  for (int i = 0; i < kRows / 4; ++i) { run.m[i] = neg_inf(); run.l[i] = 0.f; }
+  for (int i = 0; i < kRows / 4; ++i) { run.m[i] = -FLT_MAX; run.l[i] = 0.f; }
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -212,9 +213,9 @@ attend_simt_kernel(AttendArgs a) {
         n[j] = there ? min(8, max(0, w.seen - pos[j])) : 0;
         half[j] = (long long)w.begin + pos[j];
       }
-      const bool masked = !kPages && w.own == 0 && t * kTile + kTile > w.limit(s.G, 0);
+      const bool masked = !kPages && w.own == 0 && t * kTile + kTile > w.limit(0);
       tile<F>(a.K, a.V, k_base, v_base, ks_base, vs_base, half, n, s.D, w.rows, a.scale_log2, q_sh, p_all[warp], run, lane, masked,
-              [&](int key, int r) { return t * kTile + key < w.limit(s.G, r); });
+              [&](int key, int r) { return t * kTile + key < w.limit(r); });
     } else {
       const int first = (t - cached) * kTile;
 #pragma unroll
@@ -225,7 +226,7 @@ attend_simt_kernel(AttendArgs a) {
       const CacheView kn{a.K_new.ptr, a.K_new.dtype, a.K_new.sl, a.K_new.st, a.K_new.sh, nullptr, 0, 0, 0};
       const CacheView vn{a.V_new.ptr, a.V_new.dtype, a.V_new.sl, a.V_new.st, a.V_new.sh, nullptr, 0, 0, 0};
       tile<FQ>(kn, vn, w.layer * kn.sl + w.hk * kn.sh, w.layer * vn.sl + w.hk * vn.sh, 0, 0, half, n, s.D, w.rows, a.scale_log2, q_sh,
-               p_all[warp], run, lane, true, [&](int key, int r) { return sees_new(a, w, w.token(s.G, r), first + key); });
+               p_all[warp], run, lane, true, [&](int key, int r) { return sees_new(a, w, w.token(r), first + key); });
     }
   }
   // the warps' parts, added up one warp after the other
@@ -235,51 +236,26 @@ attend_simt_kernel(AttendArgs a) {
     for (int d = 4; d < 32; d <<= 1) run.l[i] += __shfl_xor_sync(kAll, run.l[i], d);
     if (g == 0) warp_part[warp][2 * c + i] = Part{run.m[i], run.l[i], run.m[i], 0.f};
   }
-  __syncthreads();
-  if (tid < kRows) {
-    float m = neg_inf(), l = 0.f;
-    for (int k = 0; k < kWarps; ++k) m = fmaxf(m, warp_part[k][tid].m);
-    for (int k = 0; k < kWarps; ++k) { const Part& p = warp_part[k][tid]; l += p.l == 0.f ? 0.f : p.l * exp2f(p.m - reference(m)); }
-    part[tid] = Part{m, l, reference(m), 0.f};
-  }
-  __syncthreads();
-  for (int k = 0; k < kWarps; ++k) {
-    if (warp == k) {
+  float* o = reinterpret_cast<float*>(dyn_sh);
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        const float f = exp2f(warp_part[k][r].m - part[r].m2);
+  for (int r = 0; r < kRows; ++r)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int d = 128 * b + 4 * lane;
-          if (d < s.D) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float v = warp_part[k][r].l == 0.f ? 0.f : run.o[b][r][i] * f;
-              o_sh[r * kMaxD + d + i] = k ? o_sh[r * kMaxD + d + i] + v : v;
-            }
-          }
-        }
-      }
-    }
-    __syncthreads();
-  }
-  join_and_write<FQ, kWarps * 32>(a, w, cluster, n_blk, rank, o_sh, kMaxD, part, factor);
+    for (int b = 0; b < 2; ++b)
+      if (128 * b + 4 * lane < s.D)
+        *reinterpret_cast<float4*>(o + (warp * kRows + r) * kMaxD + 128 * b + 4 * lane) = make_float4(run.o[b][r][0], run.o[b][r][1], run.o[b][r][2], run.o[b][r][3]);
+  join_and_write<FQ, kWarps, kRows, kMaxD>(a, w, cluster, n_blk, rank, o, kMaxD, warp_part[0], &recv);
 }
 
 template <int FQ, int F, bool kPages>
 int launch_one(AttendArgs& a, cudaStream_t stream) {
   auto kern = attend_simt_kernel<FQ, F, kPages>;
   const Shape& s = a.s;
-  const long long rows = (long long)(kPages ? 1 : a.fresh.most) * s.G;
-  a.row_blocks = (int)((rows + kRows - 1) / kRows);
-  const long long units = (long long)s.n_layers * (kPages ? a.fresh.total : s.n_seqs) * s.Hkv * a.row_blocks;
-  const long long keys = kPages ? (long long)(a.pages.budget < a.pages.max_pages ? a.pages.budget : a.pages.max_pages) * a.pages.page_size
-                                : (long long)s.max_seqlen + (a.K_new.ptr ? a.fresh.most : 0);
-  const int n_blk = cluster_size(units, (int)((keys + kTile - 1) / kTile), kWarps, 8, 4 * sm_count());
-  if (units * n_blk > 0x7FFFFFFFLL) return KVCRUSH_ERR_UNSUPPORTED;
-  const size_t dyn = kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0;
-  if (kPages && allow_dynamic_smem(kern, (int)page_mem_bytes(kMaxPagesPerSeq, kMaxPagesPerSeq, kMaxD)) != KVCRUSH_OK) return KVCRUSH_ERR_CUDA;
-  return launch_chained(kern, dim3((unsigned)(units * n_blk)), dim3(kWarps * 32), dyn, stream, n_blk, a);
+  const int n_blk = cluster_size(attend_units(a, kRows), attend_tiles(a), kWarps, 8, 4 * sm_count());
+  dim3 grid;
+  if (!attend_grid(a, kRows, n_blk, &grid)) return KVCRUSH_ERR_UNSUPPORTED;
+  const size_t dyn = kOBytes + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
+  if (allow_dynamic_smem(kern, kOBytes + (kPages ? (int)page_mem_bytes(kMaxPagesPerSeq, kMaxPagesPerSeq, kMaxD) : 0)) != KVCRUSH_OK) return KVCRUSH_ERR_CUDA;
+  return launch_chained(kern, grid, dim3(kWarps * 32), dyn, stream, n_blk, a);
 }
 
 template <int FQ, int F>

@@ -257,7 +257,7 @@ struct AttendArgs {
   const int32_t* row_count;
   float* lse;
   float scale_log2;
-  int row_blocks;                  // blocks of query rows of a unit of work
+  uint32_t group_magic;            // row / G = row * group_magic >> 32 (G > 1)
   PageChoice pages;                  // page_size 0: every row is read
 };
 // float32 queries, caches of any type
