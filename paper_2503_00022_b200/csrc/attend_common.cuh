@@ -191,39 +191,84 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
       }
     }
     __syncthreads();
-    // the want-th largest key, eight bits at a time, and how many of its equals belong to the chosen ones
-    unsigned long long prefix = 0, mask = 0;
-    int left = want;
-    for (int shift = 56; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kThreads) mem.count[i] = 0;
-      __syncthreads();
-      for (int i = tid; i < n_pages; i += kThreads)
-        if ((mem.keys[i] & mask) == prefix) atomicAdd(mem.count + (int)(mem.keys[i] >> shift & 255u), 1);
-      __syncthreads();
-      if (warp == 0) {                       // lane: eight digits, from the top
-        int c[8], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { c[i] = mem.count[255 - (lane * 8 + i)]; sum += c[i]; }
-        int before = sum;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(kAll, before, d); if (lane >= d) before += o; }
-        before -= sum;
-        if (before < left && before + sum >= left) {
-          int i = 0;
-          while (before + c[i] < left) before += c[i++];
-          mem.count[256] = 255 - (lane * 8 + i);
-          mem.count[257] = left - before;
-        }
-      }
-      __syncthreads();
-      prefix |= (unsigned long long)mem.count[256] << shift;
-      mask |= 255ull << shift;
-      left = mem.count[257];
+    // The want-th largest key.  Scores differ little in their leading bits, so the search starts at the highest bit in which
+    // any two keys differ (those read by decree apart) and goes on eight bits at a time until the keys that share the
+    // bits found so far are all taken.
+    unsigned long long both = ~0ull, any = 0ull;
+    int decreed = 0;
+    for (int i = tid; i < n_pages; i += kThreads) {
+      const unsigned long long k = mem.keys[i];
+      if (k == kDecreed) ++decreed; else { both &= k; any |= k; }
     }
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      both &= __shfl_xor_sync(kAll, both, d);
+      any |= __shfl_xor_sync(kAll, any, d);
+      decreed += __shfl_xor_sync(kAll, decreed, d);
+    }
+    unsigned long long* bits = reinterpret_cast<unsigned long long*>(mem.count);   // [2][kWarps]
+    if (lane == 0) { bits[warp] = both; bits[kWarps + warp] = any; mem.count[264 + warp] = decreed; }
+    __syncthreads();
+    both = ~0ull; any = 0ull; decreed = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) { both &= bits[i]; any |= bits[kWarps + i]; decreed += mem.count[264 + i]; }
+    __syncthreads();
+    unsigned long long prefix, mask;
+    int left;
+    if (decreed >= want) {                   // only pages by decree, the lowest ones
+      prefix = kDecreed; mask = ~0ull; left = want;
+    } else {
+      const int top = 64 - __clzll(any & ~both);                     // bits below differ
+      mask = top == 64 ? 0ull : ~0ull << top;
+      prefix = both & mask;
+      left = want - decreed;
+      for (int high = top; high > 0;) {
+        const int shift = max(0, high - 8);
+        const unsigned digits = (1u << (high - shift)) - 1u;
+        for (int i = tid; i < 256; i += kThreads) mem.count[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < n_pages; i += kThreads) {
+          const unsigned long long k = mem.keys[i];
+          if (k != kDecreed && (k & mask) == prefix) atomicAdd(mem.count + ((unsigned)(k >> shift) & digits), 1);
+        }
+        __syncthreads();
+        if (warp == 0) {                     // lane: eight digits, from the top
+          int c[8], sum = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) { c[i] = mem.count[255 - (lane * 8 + i)]; sum += c[i]; }
+          int before = sum;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(kAll, before, d); if (lane >= d) before += o; }
+          before -= sum;
+          if (before < left && before + sum >= left) {
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              if (!found && before + c[i] >= left) {
+                mem.count[256] = 255 - (lane * 8 + i);
+                mem.count[257] = left - before;
+                mem.count[258] = c[i];
+                found = true;
+              }
+              before += c[i];
+            }
+          }
+        }
+        __syncthreads();
+        prefix |= (unsigned long long)mem.count[256] << shift;
+        mask |= (unsigned long long)digits << shift;
+        left = mem.count[257];
+        if (mem.count[258] == left) break;
+        high = shift;
+      }
+    }
+    const bool by_decree = decreed < want;   // those come on top of what the search found
     // chosen pages in order: thread t looks at a run of pages; equals are taken from the front
     const int run = (n_pages + kThreads - 1) / kThreads, lo = min(n_pages, tid * run), hi = min(n_pages, lo + run);
     int above = 0, equal = 0;
-    for (int i = lo; i < hi; ++i) { above += mem.keys[i] > prefix; equal += mem.keys[i] == prefix; }
+    auto is_above = [&](unsigned long long k) { return k == kDecreed ? by_decree : (k & mask) > prefix; };
+    auto is_equal = [&](unsigned long long k) { return k == kDecreed ? !by_decree : (k & mask) == prefix; };
+    for (int i = lo; i < hi; ++i) { above += is_above(mem.keys[i]); equal += is_equal(mem.keys[i]); }
     int sa = above, se = equal;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -236,8 +281,8 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
     for (int i = 0; i < warp; ++i) { sa += mem.count[264 + i]; se += mem.count[264 + 16 + i]; }
     int at = sa + min(se, left);
     for (int i = lo; i < hi; ++i) {
-      const bool eq = mem.keys[i] == prefix;
-      if (mem.keys[i] > prefix || (eq && se < left)) mem.chosen[at++] = i;
+      const bool eq = is_equal(mem.keys[i]);
+      if (is_above(mem.keys[i]) || (eq && se < left)) mem.chosen[at++] = i;
       se += eq;
     }
   } else {

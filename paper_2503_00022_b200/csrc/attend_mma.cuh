@@ -539,7 +539,7 @@ __device__ __forceinline__ void add_tile(uint32_t stage, const Halves& h, int D,
 // ---- the kernel ---------------------------------------------------------------------------------------------------
 
 // Byte offsets in dynamic shared memory.  The warps' outputs take the place of the rings at the end.
-template <int F, int FQ, int DP, int NB, int kWarps>
+template <int F, int FQ, int DP, int NB, int kWarps, bool kPages>
 struct Mem {
   static constexpr int kRows = 8 * NB;
   static constexpr int kQStride = DP * 2 + 16, kOStride = DP + 4;
@@ -550,10 +550,10 @@ struct Mem {
   static constexpr int kRecv = kPart + kWarps * kRows * (int)sizeof(Part);
   static constexpr int kRing = (kRecv + (int)sizeof(Received<kRows, DP>) + 127) / 128 * 128;
   static constexpr int kO = kRing;
-  // At most 96 KB of rings a block, less where two blocks would not fit an SM: as many stages as that holds, two at least, and
+  // At most 96 KB of rings a block, less where two blocks would not fit an SM (the choice of pages needs room too): as many stages as that holds, two at least, and
   // room for a tile of 16-bit new tokens.
   static constexpr int kStageBytes = (Stage<F, DP>::kBytes + 127) / 128 * 128;
-  static constexpr int kWarpBytes = (kRing > 16 * 1024 ? 112 * 1024 - kRing : 96 * 1024) / kWarps;
+  static constexpr int kWarpBytes = (kPages ? 64 * 1024 : kRing > 16 * 1024 ? 112 * 1024 - kRing : 96 * 1024) / kWarps;
   static constexpr int kStages = kWarpBytes / kStageBytes < 2 ? 2 : kWarpBytes / kStageBytes > 6 ? 6 : kWarpBytes / kStageBytes;
   static constexpr int kNewBytes = kQuantized<F> ? Stage<FQ, DP>::kBytes : 0;
   static constexpr int kRingBytes = kStages * kStageBytes > kNewBytes ? kStages * kStageBytes : kNewBytes;
@@ -564,7 +564,7 @@ struct Mem {
 template <int F, int FQ, int DP, int NB, int kWarps, int kBlocks, bool kPages>
 __global__ void __launch_bounds__(kWarps * 32, kBlocks)
 attend_kernel(AttendArgs a) {
-  using M = Mem<F, FQ, DP, NB, kWarps>;
+  using M = Mem<F, FQ, DP, NB, kWarps, kPages>;
   using L = Layout<F, DP>;
   constexpr bool kScaled = kQuantized<F>;
   constexpr int A = kArith<F, FQ>, kRows = M::kRows;
@@ -890,9 +890,9 @@ int largest_cluster(Kernel kern, int threads, size_t dyn, std::atomic<int>* know
 template <int F, int FQ, int DP, int NB, bool kPages>
 int launch_one(AttendArgs& a, cudaStream_t stream) {
   // Two blocks an SM: a chip has room for 14 clusters of 16 then, with one only for 7.
-  constexpr int kWarps = NB * DP <= 128 && (kQuantized<F> || DP == 64) ? 8 : 4, kBlocks = Mem<F, FQ, DP, NB, kWarps>::kEnd <= 113 * 1024 ? 2 : 1;
+  constexpr int kWarps = NB * DP <= 128 && (kQuantized<F> || DP == 64) ? 8 : 4, kBlocks = Mem<F, FQ, DP, NB, kWarps, kPages>::kEnd <= 113 * 1024 ? 2 : 1;
   auto kern = attend_kernel<F, FQ, DP, NB, kWarps, kBlocks, kPages>;
-  using M = Mem<F, FQ, DP, NB, kWarps>;
+  using M = Mem<F, FQ, DP, NB, kWarps, kPages>;
   const Shape& s = a.s;
   constexpr int most = (M::kEnd + 15) / 16 * 16;
   const size_t dyn = most + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
