@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -97,12 +98,12 @@ def lib() -> ctypes.CDLL:
         L.kvcrush_select_pages.argtypes = [P, vp, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp, vp]
         L.kvcrush_compact_pages.argtypes = [P, T, T, i32, vp, vp, i64, T, T, vp, vp]
         L.kvcrush_signature_static.argtypes = [P, vp, vp, vp, vp, vp]
-        C, N = ctypes.POINTER(ScalesStruct), ctypes.POINTER(NewTokensStruct)
-        L.kvcrush_quantize.argtypes = [P, T, T, vp, vp, i64, vp, vp, T, C, T, C, vp, vp]
-        L.kvcrush_dequantize.argtypes = [P, T, C, T, C, vp, vp, i64, vp, vp, T, T, vp, vp]
-        L.kvcrush_attend.argtypes = [P, N, T, T, C, T, C, T, T, vp, vp, T, vp, vp, vp]
-        L.kvcrush_page_bounds.argtypes = [P, T, i32, i32, vp, vp, T, T, vp, vp]
-        L.kvcrush_attend_pages.argtypes = [P, N, T, T, C, T, C, i32, T, T, i32, i32, i32, vp, vp, vp, vp, T, vp, vp, vp]
+        # descriptors of these go as addresses or packed bytes, see _packed
+        L.kvcrush_quantize.argtypes = [vp] * 5 + [i64] + [vp] * 8
+        L.kvcrush_dequantize.argtypes = [vp] * 7 + [i64] + [vp] * 6
+        L.kvcrush_attend.argtypes = [vp] * 15
+        L.kvcrush_page_bounds.argtypes = [vp, vp, i32, i32] + [vp] * 6
+        L.kvcrush_attend_pages.argtypes = [vp] * 7 + [i32, vp, vp, i32, i32, i32] + [vp] * 8
         L.kvcrush_strerror.argtypes = [i32]
         L.kvcrush_strerror.restype = ctypes.c_char_p
         L.kvcrush_version.argtypes = []
@@ -175,6 +176,7 @@ class Problem:
         self.struct = ProblemStruct(
             n_layers, self.n_seqs, n_q_heads, n_kv_heads, head_dim, self.total_tokens, self.max_seqlen,
             int(causal), float(softmax_scale), int(query_window), self.cu_host.ctypes.data, int(self.cu_dev.data_ptr()))
+        self.address = ctypes.addressof(self.struct)
 
     @property
     def ref(self):
@@ -191,7 +193,7 @@ def tensor_struct(t) -> TensorStruct:
 class QuantTensor:
     """K or V of a quantised cache: codes [layers, rows, heads, D bytes (INT4: D/2)] (uint8) and float32 scales
     [layers, rows, heads] (INT4: [layers, rows, heads, 2], scale and zero), both with any strides but along the last axis.
-    Owns nothing but the two tensors and their descriptors."""
+    Owns nothing but the two tensors and their descriptors, which are taken when it is made."""
 
     def __init__(self, codes, scales, format: int):
         import torch
@@ -201,8 +203,8 @@ class QuantTensor:
         self.codes, self.scales, self.format = codes, scales, int(format)
         per_byte = 2 if format == INT4 else 1
         self.head_dim = int(codes.shape[3]) * per_byte
-        self.struct = TensorStruct(codes.data_ptr(), self.format, 0, *(per_byte * x for x in codes.stride()[:3]))
-        self.scales_struct = ScalesStruct(scales.data_ptr(), *scales.stride()[:3])
+        self.refs = (_TENSOR.pack(codes.data_ptr(), self.format, 0, *(per_byte * x for x in codes.stride()[:3])),
+                     _SCALES.pack(scales.data_ptr(), *scales.stride()[:3]))
 
     @classmethod
     def empty(cls, n_layers: int, rows: int, n_heads: int, head_dim: int, format: int, device="cuda:0") -> "QuantTensor":
@@ -230,18 +232,27 @@ class NewTokens:
             assert mask.dtype == torch.int32 and mask.dim() == 2 and mask.shape[0] == self.total and mask.is_contiguous()
         self.struct = NewTokensStruct(self.total, max(self.counts, default=0), 0 if mask is None else int(mask.shape[1]), 0,
                                       self.cu_host.ctypes.data, int(self.cu_dev.data_ptr()), _ptr(mask))
-        self.ref = ctypes.byref(self.struct)
+        self.ref = ctypes.addressof(self.struct)
+
+
+# A kvcrush_tensor_t and a kvcrush_scales_t as packed bytes, which ctypes passes as a pointer: 0.6 us a tensor, 1.7 us as a
+# ctypes Structure.  The calls below carry up to eight of them.
+_TENSOR, _SCALES = struct.Struct("@Pii3q"), struct.Struct("@P3q")
 
 
 def _cache_refs(t):
     """Descriptors of a tensor or a QuantTensor: values or codes, and scales or nothing."""
-    if isinstance(t, QuantTensor):
-        return ctypes.byref(t.struct), ctypes.byref(t.scales_struct)
-    return _tensor_ref(t), None
+    if type(t) is QuantTensor:
+        return t.refs
+    return _packed(t), None
 
 
-def _tensor_ref(t):
-    return None if t is None else ctypes.byref(tensor_struct(t))
+def _packed(t):
+    if t is None:
+        return None
+    sl, st, sh, one = t.stride()
+    assert one == 1, "expected [layers, tokens, heads, D] with contiguous D"
+    return _TENSOR.pack(t.data_ptr(), _dtype_codes[t.dtype] if _dtype_codes else dtype_code(t.dtype), 0, sl, st, sh)
 
 
 def kvcrush_workspace_size(problem: Problem, stage: int) -> int:
@@ -368,7 +379,7 @@ def kvcrush_quantize(problem: Problem, k, v, k_q: QuantTensor, v_q: Optional[Qua
     """Quantises rows of k and v [layers, tokens, heads, D] into k_q and v_q: kept rows (cu_kept, idx), or all of them."""
     kc, ks = _cache_refs(k_q)
     vc, vs = (None, None) if v_q is None else _cache_refs(v_q)
-    _check(lib().kvcrush_quantize(problem.ref, _tensor_ref(k), _tensor_ref(v), _ptr(cu_kept), _ptr(idx), int(total_kept),
+    _check(lib().kvcrush_quantize(problem.address, _packed(k), _packed(v), _ptr(cu_kept), _ptr(idx), int(total_kept),
                                   _ptr(in_begin), _ptr(out_begin), kc, ks, vc, vs, _ptr(status),
                                   _stream() if stream is None else stream), "kvcrush_quantize")
 
@@ -378,8 +389,8 @@ def kvcrush_dequantize(problem: Problem, k_q: QuantTensor, v_q: Optional[QuantTe
     """Reads rows of a quantised cache back into k and v."""
     kc, ks = _cache_refs(k_q)
     vc, vs = (None, None) if v_q is None else _cache_refs(v_q)
-    _check(lib().kvcrush_dequantize(problem.ref, kc, ks, vc, vs, _ptr(cu_kept), _ptr(idx), int(total_kept), _ptr(in_begin),
-                                    _ptr(out_begin), _tensor_ref(k), _tensor_ref(v), _ptr(status),
+    _check(lib().kvcrush_dequantize(problem.address, kc, ks, vc, vs, _ptr(cu_kept), _ptr(idx), int(total_kept), _ptr(in_begin),
+                                    _ptr(out_begin), _packed(k), _packed(v), _ptr(status),
                                     _stream() if stream is None else stream), "kvcrush_dequantize")
 
 
@@ -388,16 +399,16 @@ def kvcrush_attend(problem: Problem, new: NewTokens, q, k, v, out, *, k_new=None
     """Attention of new tokens q [layers, new.total, Hq, D] over a cache (tensors or QuantTensors) into out."""
     kc, ks = _cache_refs(k)
     vc, vs = _cache_refs(v)
-    _check(lib().kvcrush_attend(problem.ref, new.ref, _tensor_ref(q), kc, ks, vc, vs, _tensor_ref(k_new), _tensor_ref(v_new),
-                                _ptr(row_begin), _ptr(row_count), _tensor_ref(out), _ptr(lse), _ptr(status),
+    _check(lib().kvcrush_attend(problem.address, new.ref, _packed(q), kc, ks, vc, vs, _packed(k_new), _packed(v_new),
+                                _ptr(row_begin), _ptr(row_count), _packed(out), _ptr(lse), _ptr(status),
                                 _stream() if stream is None else stream), "kvcrush_attend")
 
 
 def kvcrush_page_bounds(problem: Problem, k, page_size: int, lo, hi, *, recent_pages: int = 0, row_begin=None, row_count=None,
                         status=None, stream: Optional[int] = None) -> None:
     """Least and largest key channels of every page (or of the last ones) into lo and hi [layers, n_seqs * max_pages, Hkv, D]."""
-    _check(lib().kvcrush_page_bounds(problem.ref, _tensor_ref(k), int(page_size), int(recent_pages), _ptr(row_begin),
-                                     _ptr(row_count), _tensor_ref(lo), _tensor_ref(hi), _ptr(status),
+    _check(lib().kvcrush_page_bounds(problem.address, _packed(k), int(page_size), int(recent_pages), _ptr(row_begin),
+                                     _ptr(row_count), _packed(lo), _packed(hi), _ptr(status),
                                      _stream() if stream is None else stream), "kvcrush_page_bounds")
 
 
@@ -407,9 +418,9 @@ def kvcrush_attend_pages(problem: Problem, new: NewTokens, q, k, v, page_size: i
     """Attention of new tokens over the `budget` pages whose bounds promise the largest logits."""
     kc, ks = _cache_refs(k)
     vc, vs = _cache_refs(v)
-    _check(lib().kvcrush_attend_pages(problem.ref, new.ref, _tensor_ref(q), kc, ks, vc, vs, int(page_size), _tensor_ref(lo),
-                                      _tensor_ref(hi), int(budget), int(keep_initial), int(keep_recent), _ptr(row_begin),
-                                      _ptr(row_count), _ptr(page_idx), _ptr(n_pages), _tensor_ref(out), _ptr(lse), _ptr(status),
+    _check(lib().kvcrush_attend_pages(problem.address, new.ref, _packed(q), kc, ks, vc, vs, int(page_size), _packed(lo),
+                                      _packed(hi), int(budget), int(keep_initial), int(keep_recent), _ptr(row_begin),
+                                      _ptr(row_count), _ptr(page_idx), _ptr(n_pages), _packed(out), _ptr(lse), _ptr(status),
                                       _stream() if stream is None else stream), "kvcrush_attend_pages")
 
 

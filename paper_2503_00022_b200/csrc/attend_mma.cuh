@@ -859,19 +859,24 @@ attend_kernel(AttendArgs a) {
 
 // ---- host -----------------------------------------------------------------------------------------------------
 
-// Largest cluster of this kernel that the device runs (write-once cache per device): 16 blocks are more than every device
-// grants.
+// Lets the kernel be launched with up to `bound` bytes of dynamic shared memory and returns the largest cluster of it that the
+// device runs, 0 where something failed (write-once cache per device; asking costs a call 1 us): 16 blocks are more than every
+// device grants.
 template <class Kernel>
-int largest_cluster(Kernel kern, int threads, size_t dyn, std::atomic<int>* known) {
+int largest_cluster(Kernel kern, int threads, int bound, std::atomic<int>* known) {
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return 8; }
-  int n = known[dev].load(std::memory_order_relaxed);
-  if (n > 0) return n;
-  n = 8;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 0; }
+  const bool cached = dev >= 0 && dev < kMaxDevices;
+  if (cached) {
+    const int n = known[dev].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+  }
+  if (allow_dynamic_smem(kern, bound) != KVCRUSH_OK) return 0;
+  int n = 8;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kMaxCluster);
   cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = dyn;
+  cfg.dynamicSmemBytes = bound;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = kMaxCluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
@@ -883,7 +888,7 @@ int largest_cluster(Kernel kern, int threads, size_t dyn, std::atomic<int>* know
     n = kMaxCluster;
   else
     cudaGetLastError();
-  known[dev].store(n, std::memory_order_relaxed);
+  if (cached) known[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 
@@ -897,9 +902,10 @@ int launch_one(AttendArgs& a, cudaStream_t stream) {
   constexpr int most = (M::kEnd + 15) / 16 * 16;
   const size_t dyn = most + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
   constexpr int bound = most + (kPages ? kMaxPagesPerSeq * 12 + 256 * 16 + 2048 : 0);
-  if (allow_dynamic_smem(kern, bound) != KVCRUSH_OK) return KVCRUSH_ERR_CUDA;
   static std::atomic<int> known[kMaxDevices];
-  const int n_blk = cluster_size(attend_units(a, M::kRows), attend_tiles(a), kWarps, largest_cluster(kern, kWarps * 32, bound, known), 2 * sm_count());
+  const int largest = largest_cluster(kern, kWarps * 32, bound, known);
+  if (largest == 0) return KVCRUSH_ERR_CUDA;
+  const int n_blk = cluster_size(attend_units(a, M::kRows), attend_tiles(a), kWarps, largest, 2 * sm_count());
   dim3 grid;
   if (!attend_grid(a, M::kRows, n_blk, &grid)) return KVCRUSH_ERR_UNSUPPORTED;
   return launch_chained(kern, grid, dim3(kWarps * 32), dyn, stream, n_blk, a);
