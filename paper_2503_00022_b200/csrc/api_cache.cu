@@ -114,6 +114,7 @@ int make_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* ne
   a->row_begin = row_begin_dev;
   a->row_count = row_count_dev;
   a->lse = lse_out_dev;
+  a->status = status_dev;
   const float scale = problem->softmax_scale != 0.f ? problem->softmax_scale : 1.f / sqrtf((float)s.D);
   a->scale_log2 = scale * 1.4426950408889634f;
   return KVCRUSH_OK;
@@ -122,6 +123,11 @@ int make_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* ne
 int dispatch_attend(const AttendArgs& a, void* stream) {
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a.Q.dtype == KVCRUSH_FP32) return launch_attend_simt(a, st);
+  if (attend_tree_fits(a)) {
+    bool taken = false;
+    const int rc = launch_attend_tree(a, &taken, st);
+    if (taken) return rc;
+  }
   switch (a.K.dtype) {
     case KVCRUSH_BF16: return launch_attend_bf16(a, st);
     case KVCRUSH_FP16: return launch_attend_fp16(a, st);

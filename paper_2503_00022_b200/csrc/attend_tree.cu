@@ -1,0 +1,457 @@
+// Attention of many query rows over a cache of 16-bit values: trees of drafted tokens and grouped heads whose rows fill a tile of
+// tcgen05.
+//
+// With 128 query rows a cached key costs 4 * 128 * D operations for its 4 D bytes, so that both the tensor cores and HBM have
+// work.  A block takes 128 query rows (TMEM lane = row) of one (layer, sequence, KV head) and a share of the keys, in tiles of
+// 64: S = Q K^T, the softmax in registers of the thread that owns the row, P back to TMEM as the left operand of O += P V, whose
+// right operand V is read as it lies in memory (its channels are the fast axis).  The queries stay in shared memory, keys and
+// values come by TMA; S is double-buffered (P takes the first half of its own S), so that the product of the next tile runs
+// while this one's softmax does, and two blocks share an SM.  Weights may exceed 1: the reference of a row moves only where
+// a logit is 2^8 above it, and only then the output in TMEM is scaled.
+// Whole tiles that every row sees go this way.  What is left - the tail of the cache, rows of the cache that only later
+// tokens see, and the new tokens with their mask - is a few keys for each block of the cluster, which the threads of the rows
+// add one key at a time, so that keys that a row does not see have no influence whatever they hold.
+// Tree of 63 tokens x 4 heads over 32768 rows x 8 KV heads of 128: see the figures at launch_attend_tree.
+#include "attend_common.cuh"
+#include "tc_ptx.cuh"
+
+namespace kvc {
+
+namespace {
+
+using namespace att;
+using namespace fmt;
+
+constexpr int kRows = 128;                   // query rows of a block
+constexpr int kKeys = 64;                    // keys of a tile
+constexpr int kThreads = 256;                // producer, issuer, two helpers, four softmax warps
+constexpr int kTreeCluster = 8;
+constexpr int kExtra = 8;                    // keys added at a time by the rows' threads
+constexpr float kSlackLog2 = 8.f;
+constexpr uint32_t kPolls = tc::kWaitPolls;
+
+template <int DP>
+struct TreeMem {
+  static constexpr int kBlocks = DP / 64;                               // of 64 channels: 128-byte rows
+  static constexpr int kStages = DP == 128 ? 2 : 4;
+  static constexpr int kQ = 0, kQBytes = kBlocks * kRows * 128;
+  static constexpr int kTileBytes = kBlocks * kKeys * 128;              // keys or values of a stage
+  static constexpr int kRing = kQ + kQBytes;
+  static constexpr int kRecvO = kRing;                                  // outputs of the peers, when the ring is done with
+  static constexpr int kRecvPart = kRing + 2 * kStages * kTileBytes + 256;
+  static constexpr int kAux = kRecvPart + kTreeCluster * kRows * 8;
+  static constexpr int kEnd = kAux + 256;
+  static_assert(kRows * DP * 4 + kTreeCluster * 16 <= 2 * kStages * kTileBytes + 256, "room for the peers' outputs");
+  static_assert(kEnd <= 112 * 1024, "two blocks an SM");
+};
+struct TreeAux {
+  unsigned long long k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_ready[2], o_done, drain;
+  uint32_t tmem;
+  int abort_flag;
+};
+static_assert(sizeof(TreeAux) <= 256, "auxiliary memory");
+
+// Descriptor of 16 keys x 64 or 128 channels of values: rows of 64 channels (128 bytes, 128-byte swizzle), eight keys 1024 bytes
+// apart, blocks of 64 channels kKeys rows apart.
+__device__ __forceinline__ uint64_t values_desc(uint32_t addr) {
+  return tc::smem_desc_sw128(addr) & ~(0x3FFFull << 16) | (uint64_t)(kKeys * 128 >> 4) << 16;
+}
+__device__ __forceinline__ void umma_p(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <int FQ>
+__device__ __forceinline__ void widen8(const uint4& v, float (&x)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = FQ == KVCRUSH_BF16 ? unpack_bf16(w[i]) : unpack_fp16(w[i]);
+    x[2 * i] = f.x; x[2 * i + 1] = f.y;
+  }
+}
+
+template <int FQ, int DP>
+__global__ void __launch_bounds__(kThreads, 2)
+attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, AttendArgs a) {
+  using M = TreeMem<DP>;
+  using tc::mbar_wait;
+  extern __shared__ __align__(1024) unsigned char sh[];
+  chain_wait();
+  chain_trigger();
+  cg::cluster_group cluster = cg::this_cluster();
+  const int n_blk = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const Shape& s = a.s;
+  Unit w;
+  if (!unit_of<false>(a, kRows, w)) return;
+  TreeAux* aux = reinterpret_cast<TreeAux*>(sh + M::kAux);
+  const uint32_t base = tc::smem_u32(sh);
+  if (tid == 0) {
+    for (int i = 0; i < M::kStages; ++i) {
+      tc::mbar_init(tc::smem_u32(&aux->k_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->k_empty[i]), 1);
+      tc::mbar_init(tc::smem_u32(&aux->v_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->v_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) { tc::mbar_init(tc::smem_u32(&aux->s_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->p_ready[i]), kRows); }
+    tc::mbar_init(tc::smem_u32(&aux->o_done), 1);
+    tc::mbar_init(tc::smem_u32(&aux->drain), 1);
+    aux->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(tc::smem_u32(&aux->tmem), 256);
+    tc::tmem_relinquish();
+  }
+  // queries: rows of 128 bytes, 128-byte swizzle, as TMA would lay them out
+  for (int e = tid; e < kRows * (DP / 8); e += kThreads) {
+    const int r = e / (DP / 8), c = e % (DP / 8);
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (r < w.rows && c * 8 < s.D)
+      v = __ldg(reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(a.Q.ptr) +
+              bytes_of<FQ>(w.layer * a.Q.sl + (w.first + w.token(r)) * a.Q.st + (w.hk * s.G + w.head(r)) * a.Q.sh + c * 8)));
+    *reinterpret_cast<uint4*>(sh + M::kQ + (c >> 3) * kRows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+  }
+  proxy_fence();
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  volatile int* abort_flag = &aux->abort_flag;
+  const uint32_t tmem = aux->tmem, tmem_o = tmem + 128;
+
+  const int full = (w.own ? w.seen : w.limit(0)) / kKeys;             // tiles that every row sees
+  const int per = (full + n_blk - 1) / n_blk, lo = min(full, rank * per), n = min(full, lo + per) - lo;
+  const int tail = w.seen - full * kKeys, extra = tail + w.own;       // keys that are added one by one
+  const int per_extra = (extra + n_blk - 1) / n_blk, e_lo = min(extra, rank * per_extra), e_hi = min(extra, e_lo + per_extra);
+  float m = -FLT_MAX, l = 0.f;
+  bool has_o = n > 0;
+
+  if (warp == 0) {
+    int issued = 0;
+    if (lane == 0) {
+      for (; issued < n; ++issued) {
+        const int st = issued % M::kStages, round = issued / M::kStages;
+        const int row = w.begin + (lo + issued) * kKeys;
+        const uint32_t kb = tc::smem_u32(&aux->k_full[st]), vb = tc::smem_u32(&aux->v_full[st]);
+        const uint32_t kd = base + M::kRing + st * 2 * M::kTileBytes, vd = kd + M::kTileBytes;
+        if (round > 0 && !mbar_wait(tc::smem_u32(&aux->k_empty[st]), (round - 1) & 1, abort_flag, kPolls)) break;
+        tc::mbar_expect_tx(kb, M::kTileBytes);
+        for (int b = 0; b < M::kBlocks; ++b) tc::tma_load_4d(kd + b * kKeys * 128, &map_k, kb, b * 64, row, w.hk, w.layer);
+        if (round > 0 && !mbar_wait(tc::smem_u32(&aux->v_empty[st]), (round - 1) & 1, abort_flag, kPolls)) {
+          for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(kb, round & 1); ++i) {}
+          break;
+        }
+        tc::mbar_expect_tx(vb, M::kTileBytes);
+        for (int b = 0; b < M::kBlocks; ++b) tc::tma_load_4d(vd + b * kKeys * 128, &map_v, vb, b * 64, row, w.hk, w.layer);
+      }
+      // nothing may be in flight when the block goes on: the last round's copies have landed (at once, but after a wait ran out)
+      for (int t = max(0, issued - M::kStages); t < issued; ++t) {
+        const int st = t % M::kStages, parity = (t / M::kStages) & 1;
+        for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(tc::smem_u32(&aux->k_full[st]), parity); ++i) {}
+        for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(tc::smem_u32(&aux->v_full[st]), parity); ++i) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0 && n > 0) {
+      constexpr uint32_t idesc_s = tc::make_idesc(kRows, kKeys, FQ == KVCRUSH_BF16);
+      constexpr uint32_t idesc_o = tc::make_idesc(kRows, DP, FQ == KVCRUSH_BF16) | 1u << 16;      // right operand: channels are the fast axis
+      auto product_s = [&](int t) {
+        const int st = t % M::kStages;
+        // S takes the place of the weights of two tiles before, which that tile's product has read
+        if (t >= 2 && !mbar_wait(tc::smem_u32(&aux->o_done), t & 1, abort_flag, kPolls)) return false;
+        if (!mbar_wait(tc::smem_u32(&aux->k_full[st]), (t / M::kStages) & 1, abort_flag, kPolls)) return false;
+        tc::tc_fence_after();
+        const uint32_t kd = base + M::kRing + st * 2 * M::kTileBytes;
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+          tc::umma_bf16(tmem + (t & 1) * kKeys, tc::smem_desc_sw128(base + M::kQ + (k >> 2) * kRows * 128 + (k & 3) * 32),
+                        tc::smem_desc_sw128(kd + (k >> 2) * kKeys * 128 + (k & 3) * 32), idesc_s, k > 0);
+        tc::umma_commit(tc::smem_u32(&aux->k_empty[st]));
+        tc::umma_commit(tc::smem_u32(&aux->s_full[t & 1]));
+        return true;
+      };
+      auto product_o = [&](int t) {
+        const int st = t % M::kStages;
+        if (!mbar_wait(tc::smem_u32(&aux->v_full[st]), (t / M::kStages) & 1, abort_flag, kPolls)) return false;
+        if (!mbar_wait(tc::smem_u32(&aux->p_ready[t & 1]), (t >> 1) & 1, abort_flag, kPolls)) return false;
+        tc::tc_fence_after();
+        const uint32_t vd = base + M::kRing + st * 2 * M::kTileBytes + M::kTileBytes;
+#pragma unroll
+        for (int k = 0; k < kKeys / 16; ++k)
+          umma_p(tmem_o, tmem + (t & 1) * kKeys + k * 8, values_desc(vd + k * 16 * 128), idesc_o, t > 0 || k > 0);
+        tc::umma_commit(tc::smem_u32(&aux->v_empty[st]));
+        tc::umma_commit(tc::smem_u32(&aux->o_done));
+        return true;
+      };
+      bool ok = product_s(0);
+      for (int t = 1; ok && t < n; ++t) ok = product_s(t) && product_o(t - 1);
+      if (ok) product_o(n - 1);
+      // products in flight end before TMEM is freed
+      tc::umma_commit(tc::smem_u32(&aux->drain));
+      for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(tc::smem_u32(&aux->drain), 0); ++i) {}
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    const uint32_t lanes = (uint32_t)(warp - 4) * 32u << 16;
+    const int r = (warp - 4) * 32 + lane;
+    const float scale = a.scale_log2;
+    bool ok = true;
+    auto wait = [&](unsigned long long* bar, int parity) {             // one answer for the warp
+      return (bool)__all_sync(kAll, mbar_wait(tc::smem_u32(bar), parity, abort_flag, kPolls));
+    };
+    // the output so far, times f (a factor for each row)
+    auto scale_output = [&](float f) {
+#pragma unroll 1
+      for (int c = 0; c < DP; c += 16) {
+        uint32_t v[16];
+        tc::tmem_ld16(tmem_o + lanes + c, v);
+        tc::tmem_wait16(v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+        tmem_st16(tmem_o + lanes + c, v);
+      }
+      tmem_wait_st();
+    };
+    for (int t = 0; t < n; ++t) {
+      if (!wait(&aux->s_full[t & 1], (t >> 1) & 1)) { ok = false; break; }
+      tc::tc_fence_after();
+      const uint32_t at = tmem + lanes + (t & 1) * kKeys;
+      uint32_t v[4][16];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tc::tmem_ld16(at + 16 * i, v[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tc::tmem_wait16(v[i]);
+      float top[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        top[i] = __uint_as_float(v[i][15]);
+#pragma unroll
+        for (int j = 0; j < 15; j += 3)
+          top[i] = fmaxf(top[i], tc::max3(__uint_as_float(v[i][j]), __uint_as_float(v[i][j + 1]), __uint_as_float(v[i][j + 2])));
+      }
+      const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+      if (__any_sync(kAll, most - m > kSlackLog2)) {
+        const float m_new = fmaxf(m, most), f = ex2(m - m_new);
+        m = m_new;
+        l *= f;
+        if (t > 0) {                                   // the product of the tile before may still add to the output
+          if (!wait(&aux->o_done, (t - 1) & 1)) { ok = false; break; }
+          tc::tc_fence_after();
+          scale_output(f);
+        }
+      }
+      const tc::f32x2 scale2 = tc::splat2(scale), minus_m = tc::splat2(-m);
+      tc::f32x2 sum[2] = {tc::splat2(0.f), tc::splat2(0.f)};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t p[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const uint32_t* x = &v[2 * i + (j >> 3)][2 * (j & 7)];
+          const tc::f32x2 e = tc::exp2_sfu2(tc::fma2(tc::pack2(x[0], x[1]), scale2, minus_m));
+          sum[j & 1] = tc::add2(sum[j & 1], e);
+          float e0, e1;
+          tc::unpack2(e, e0, e1);
+          p[j] = FQ == KVCRUSH_BF16 ? pack_bf16(e0, e1) : pack_fp16(e0, e1);
+        }
+        tmem_st16(at + 16 * i, p);
+      }
+      l += tc::sum4(sum);
+      tmem_wait_st();
+      tc::tc_fence_before();
+      tc::mbar_arrive(tc::smem_u32(&aux->p_ready[t & 1]));
+    }
+    if (ok && n > 0) ok = wait(&aux->o_done, (n - 1) & 1);
+    tc::tc_fence_after();
+    // keys that are added one by one
+    if (ok) {
+      const int tok = w.token(min(r, w.rows - 1)), limit = w.limit(min(r, w.rows - 1));
+      const unsigned char* kc = static_cast<const unsigned char*>(a.K.ptr) + bytes_of<FQ>(w.layer * a.K.sl + w.hk * a.K.sh);
+      const unsigned char* vc = static_cast<const unsigned char*>(a.V.ptr) + bytes_of<FQ>(w.layer * a.V.sl + w.hk * a.V.sh);
+      const unsigned char* kn = static_cast<const unsigned char*>(a.K_new.ptr) + bytes_of<FQ>(w.layer * a.K_new.sl + w.hk * a.K_new.sh);
+      const unsigned char* vn = static_cast<const unsigned char*>(a.V_new.ptr) + bytes_of<FQ>(w.layer * a.V_new.sl + w.hk * a.V_new.sh);
+#pragma unroll 1
+      for (int e0 = e_lo; e0 < e_hi; e0 += kExtra) {
+        const unsigned char *kp[kExtra], *vp[kExtra];
+        float x[kExtra];
+        bool sees[kExtra];
+        float most = -FLT_MAX;
+#pragma unroll
+        for (int j = 0; j < kExtra; ++j) {
+          const int e = min(e0 + j, e_hi - 1);
+          if (e < tail) {
+            const long long row = w.begin + full * kKeys + e;
+            kp[j] = kc + bytes_of<FQ>(row * a.K.st); vp[j] = vc + bytes_of<FQ>(row * a.V.st);
+            sees[j] = full * kKeys + e < limit;
+          } else {
+            const long long row = w.first + e - tail;
+            kp[j] = kn + bytes_of<FQ>(row * a.K_new.st); vp[j] = vn + bytes_of<FQ>(row * a.V_new.st);
+            sees[j] = sees_new(a, w, tok, e - tail);
+          }
+          sees[j] = sees[j] && e0 + j < e_hi;
+          x[j] = 0.f;
+        }
+#pragma unroll 1
+        for (int c = 0; c < s.D / 8; ++c) {
+          float q[8];
+          widen8<FQ>(*reinterpret_cast<const uint4*>(sh + M::kQ + (c >> 3) * kRows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4)), q);
+#pragma unroll
+          for (int j = 0; j < kExtra; ++j) {
+            float k[8];
+            widen8<FQ>(__ldg(reinterpret_cast<const uint4*>(kp[j]) + c), k);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[j] = fmaf(q[i], k[i], x[j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kExtra; ++j) {
+          x[j] = sees[j] ? x[j] * scale : neg_inf();
+          most = fmaxf(most, x[j]);
+        }
+        const float m_new = fmaxf(m, most), f = ex2(m - m_new);
+        m = m_new;
+        l *= f;
+#pragma unroll
+        for (int j = 0; j < kExtra; ++j) {
+          x[j] = ex2(x[j] - m);
+          l += sees[j] ? x[j] : 0.f;
+        }
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 16) {
+          uint32_t o[16];
+          if (has_o) {
+            tc::tmem_ld16(tmem_o + lanes + c, o);
+            tc::tmem_wait16(o);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[i] = has_o ? __float_as_uint(__uint_as_float(o[i]) * f) : 0u;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (c + 8 * h >= s.D) break;
+#pragma unroll
+            for (int j = 0; j < kExtra; ++j) {
+              float v[8];
+              widen8<FQ>(__ldg(reinterpret_cast<const uint4*>(vp[j]) + c / 8 + h), v);
+              if (sees[j]) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[8 * h + i] = __float_as_uint(fmaf(x[j], v[i], __uint_as_float(o[8 * h + i])));
+              }
+            }
+          }
+          tmem_st16(tmem_o + lanes + c, o);
+        }
+        tmem_wait_st();
+        has_o = true;
+      }
+    }
+  }
+  // The join: a row's thread sends its outputs to the owners of their shares.  The peers' rings are free when all have come here.
+  __syncthreads();
+  const int vec = s.D / 4, total = w.rows * vec, share = n_blk == 1 ? total : (total + n_blk - 1) / n_blk;
+  const uint32_t share_magic = 0xFFFFFFFFu / (uint32_t)share + 1u;
+  float4* recv_o = reinterpret_cast<float4*>(sh + M::kRecvO);
+  float2* recv_part = reinterpret_cast<float2*>(sh + M::kRecvPart);
+  if (n_blk > 1) { cluster_arrive(); cluster_wait(); }
+  if (warp >= 4) {
+    const uint32_t lanes = (uint32_t)(warp - 4) * 32u << 16;
+    const int r = (warp - 4) * 32 + lane;
+    if (r < w.rows)
+      for (int p = 0; p < n_blk; ++p) {
+        float2* dst = recv_part + rank * kRows + r;
+        *(n_blk > 1 ? cluster.map_shared_rank(dst, p) : dst) = make_float2(m, l);
+      }
+    has_o = __any_sync(kAll, has_o);
+#pragma unroll 1
+    for (int c = 0; c < DP; c += 16) {
+      uint32_t o[16];
+      if (has_o) {
+        tc::tmem_ld16(tmem_o + lanes + c, o);
+        tc::tmem_wait16(o);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        if (r < w.rows && c + i < s.D) {
+          const int e = r * vec + (c + i) / 4, owner = n_blk == 1 ? 0 : share == 1 ? e : (int)__umulhi((uint32_t)e, share_magic);
+          float4* dst = recv_o + rank * share + (e - owner * share);
+          *(n_blk > 1 ? cluster.map_shared_rank(dst, owner) : dst) =
+              has_o ? make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3])) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+    }
+    tc::tc_fence_before();
+  }
+  if (n_blk > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+  if (warp == 1) {
+    tc::tc_fence_after();
+    tc::tmem_dealloc(tmem, 256);
+  }
+  const int mine = rank * share;
+  for (int i = tid; i < min(share, total - mine); i += kThreads) {
+    const int e = mine + i, row = e / vec, d = (e - row * vec) * 4;
+    float top = neg_inf(), sum_l = 0.f;
+    for (int p = 0; p < n_blk; ++p) top = fmaxf(top, recv_part[p * kRows + row].x);
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < n_blk; ++p) {
+      const float2 q = recv_part[p * kRows + row];
+      const float4 v = recv_o[p * share + i];
+      const float f = ex2(q.x - top);
+      sum_l = fmaf(q.y, f, sum_l);
+      sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
+    }
+    const float inv = sum_l == 0.f ? 0.f : 1.f / sum_l;
+    const int token = w.token(row), head = w.hk * w.G + row + w.row0 - token * w.G;
+    unsigned char* op = static_cast<unsigned char*>(const_cast<void*>(a.O.ptr)) +
+        bytes_of<FQ>(w.layer * a.O.sl + (w.first + token) * a.O.st + head * a.O.sh + d);
+    if constexpr (FQ == KVCRUSH_BF16) *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+    else *reinterpret_cast<uint2*>(op) = make_uint2(pack_fp16(sum.x * inv, sum.y * inv), pack_fp16(sum.z * inv, sum.w * inv));
+    if (d == 0 && a.lse)
+      a.lse[((long long)w.layer * s.Hq + head) * a.fresh.total + w.first + token] = sum_l == 0.f ? neg_inf() : (top + log2f(sum_l)) * 0.6931471805599453f;
+  }
+  if (tid == 0 && *abort_flag) report(a.status, KVCRUSH_DEV_TIMEOUT, KID_ATTEND_TREE, (int)blockIdx.x, 0);
+}
+
+template <int FQ, int DP>
+int launch_one(const AttendArgs& a, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
+  using M = TreeMem<DP>;
+  auto kern = attend_tree_kernel<FQ, DP>;
+  if (allow_dynamic_smem(kern, M::kEnd) != KVCRUSH_OK) return KVCRUSH_ERR_CUDA;
+  const int tiles = (a.s.max_seqlen + kKeys - 1) / kKeys;
+  const int n_blk = cluster_size(attend_units(a, kRows), tiles, 2, kTreeCluster, 2 * sm_count());
+  dim3 grid;
+  if (!attend_grid(a, kRows, n_blk, &grid)) return KVCRUSH_ERR_UNSUPPORTED;
+  return launch_chained(kern, grid, dim3(kThreads), M::kEnd, stream, n_blk, mk, mv, a);
+}
+
+}  // namespace
+
+bool attend_tree_fits(const AttendArgs& a) {
+  const long long rows = (long long)a.fresh.most * a.s.G;
+  return a.pages.page_size == 0 && (a.K.dtype == KVCRUSH_BF16 || a.K.dtype == KVCRUSH_FP16) && a.s.D <= 128 && rows > 32 &&
+         a.s.max_seqlen >= 2 * kKeys && a.scale_log2 > 0.f;
+}
+
+int launch_attend_tree(const AttendArgs& a, bool* taken, cudaStream_t stream) {
+  CUtensorMap mk, mv;
+  const TensorView k{a.K.ptr, a.K.dtype, a.K.sl, a.K.st, a.K.sh}, v{a.V.ptr, a.V.dtype, a.V.sl, a.V.st, a.V.sh};
+  *taken = a.s.T > 0 && tc::make_map(&mk, k, a.s.D, a.s.T, a.s.Hkv, a.s.n_layers, kKeys) && tc::make_map(&mv, v, a.s.D, a.s.T, a.s.Hkv, a.s.n_layers, kKeys);
+  if (!*taken) return KVCRUSH_OK;
+  if (a.K.dtype == KVCRUSH_BF16) return a.s.D <= 64 ? launch_one<KVCRUSH_BF16, 64>(a, mk, mv, stream) : launch_one<KVCRUSH_BF16, 128>(a, mk, mv, stream);
+  return a.s.D <= 64 ? launch_one<KVCRUSH_FP16, 64>(a, mk, mv, stream) : launch_one<KVCRUSH_FP16, 128>(a, mk, mv, stream);
+}
+
+}  // namespace kvc

@@ -26,7 +26,7 @@ struct TensorView {
 inline int elt_bytes(int dtype) { return dtype == KVCRUSH_FP32 ? 4 : 2; }
 
 // kernel ids written to status[1]
-enum KernelId { KID_SCORE_LSE = 1, KID_SCORE_COLSUM = 2, KID_KMEANS = 3, KID_SCORE_WINDOW = 4 };
+enum KernelId { KID_SCORE_LSE = 1, KID_SCORE_COLSUM = 2, KID_KMEANS = 3, KID_SCORE_WINDOW = 4, KID_ATTEND_TREE = 5 };
 
 __device__ __forceinline__ void report(int32_t* status, int code, int kid, int a, int b) {
   if (atomicCAS(status, 0, code) == 0) {
@@ -257,6 +257,7 @@ struct AttendArgs {
   const int32_t* row_count;
   float* lse;
   float scale_log2;
+  int32_t* status;
   uint32_t group_magic;            // row / G = row * group_magic >> 32 (G > 1)
   PageChoice pages;                  // page_size 0: every row is read
 };
@@ -268,6 +269,10 @@ int launch_attend_fp16(AttendArgs a, cudaStream_t stream);
 int launch_attend_int8(AttendArgs a, cudaStream_t stream);
 int launch_attend_e4m3(AttendArgs a, cudaStream_t stream);
 int launch_attend_int4(AttendArgs a, cudaStream_t stream);
+// Many query rows over a cache of 16-bit values on tcgen05.  attend_tree_fits: does the problem suit it; *taken: could the cache be
+// described to the TMA unit (otherwise nothing was launched).
+bool attend_tree_fits(const AttendArgs& a);
+int launch_attend_tree(const AttendArgs& a, bool* taken, cudaStream_t stream);
 
 int launch_page_bounds(const Shape& s, const TensorView& K, int page_size, int recent_pages, const int32_t* row_begin,
                        const int32_t* row_count, const TensorView& lo, const TensorView& hi, cudaStream_t stream);

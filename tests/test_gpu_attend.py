@@ -349,3 +349,74 @@ def test_no_new_tokens_and_empty_caches(B):
     c.run(B.NewTokens((2, 0)))
     c.check(lambda l, s, i, h: ([], []))
     B.kvcrush_attend(c.prob, B.NewTokens((0, 0)), c.q, c.k, c.v, c.out, status=c.status)
+
+
+TREES = [
+    # type, D, query heads, KV heads, cached rows, new tokens, layers
+    ("bf16", 128, 8, 2, (700, 130, 64, 5), (20, 33, 63, 9), 1),
+    ("fp16", 64, 16, 2, (1000, 0, 333), (5, 40, 7), 2),
+    ("bf16", 96, 4, 1, (257,), (100,), 1),
+    ("fp16", 40, 33, 1, (128, 127), (1, 4), 1),
+    ("bf16", 128, 64, 1, (5000,), (3,), 1),
+    ("bf16", 64, 2, 2, (640,), (300,), 1),
+]
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,lens,counts,layers", TREES)
+@pytest.mark.parametrize("layout", [None, TL.strided, TL.by_head])
+def test_tiles_of_query_rows(B, dtype, D, Hq, Hkv, lens, counts, layers, layout):
+    """Rows that fill tiles of 128: trees, chains, tokens at the end of the cache; tails, short sequences, several tiles of rows."""
+    bits, sees = TL.tree_bits(D, counts, (max(counts) + 31) // 32, empty_row=True)
+    c = Case(B, dtype, None, D, Hq, Hkv, lens, counts, own=True, seed=D + Hq, layers=layers, layout=layout)
+    c.run(B.NewTokens(counts, mask=_dev(bits)))
+    c.check(lambda l, s, i, h: (np.arange(c.cu[s], c.cu[s + 1]), np.flatnonzero(sees[s][i])))
+    c.kn = c.vn = None
+    c.run(B.NewTokens(counts))
+    c.check(lambda l, s, i, h: (np.arange(c.cu[s], c.cu[s] + max(0, lens[s] - counts[s] + 1 + i)), []))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_unseen_rows_have_no_influence_on_tiles(B, dtype):
+    lens, counts = (300, 170), (40, 36)
+    bits, sees = TL.tree_bits(78, counts, 2, empty_row=True)
+    c = Case(B, dtype, None, 64, 4, 2, lens, counts, own=True, seed=23)
+    c.vn[0, 20, :, 3] = float("nan")
+    c.kn[0, 30, 0, 0] = float("nan")
+    c.vn[0, 60, 1] = float("inf")
+    c.run(B.NewTokens(counts, mask=_dev(bits)))
+    with np.errstate(invalid="ignore"):
+        c.check(lambda l, s, i, h: (np.arange(c.cu[s], c.cu[s + 1]), np.flatnonzero(sees[s][i])))
+    c = Case(B, dtype, None, 64, 4, 2, lens, counts, seed=24)
+    c.v[0, 290], c.k[0, 280, 0], c.v[0, 465, 1, 5] = float("nan"), float("nan"), float("inf")
+    c.k64, c.v64 = TL.numpy64(c.k), TL.numpy64(c.v)
+    c.run(B.NewTokens(counts))
+    with np.errstate(invalid="ignore"):
+        c.check(lambda l, s, i, h: (np.arange(c.cu[s], c.cu[s] + lens[s] - counts[s] + 1 + i), []))
+    # rows behind the counts, and what one sequence's rows hold, stay out of the others
+    c = Case(B, dtype, None, 64, 4, 2, (320, 320), (20, 20), own=True, seed=25)
+    c.k[0, 300:320], c.v[0, 300:320] = float("nan"), float("inf")
+    c.run(B.NewTokens((20, 20)), row_begin=_dev(np.asarray([[0, 320]], dtype=np.int32)), row_count=_dev(np.asarray([[300, 200]], dtype=np.int32)))
+    c.check(lambda l, s, i, h: (np.arange((0, 320)[s], (300, 520)[s]), np.arange(i + 1)))
+
+
+def test_growing_maxima_on_tiles(B):
+    """Keys whose logits grow along the cache, so that the reference of the weights has to move often."""
+    import torch
+    c = Case(B, "bf16", None, 128, 8, 1, (2000,), (10,), own=True, seed=26)
+    c.k *= torch.linspace(0.1, 12.0, 2000, device="cuda:0").view(1, -1, 1, 1).to(c.k.dtype)
+    c.k64 = TL.numpy64(c.k)
+    c.run(B.NewTokens((10,)))
+    c.check(lambda l, s, i, h: (np.arange(2000), np.arange(i + 1)))
+
+
+def test_negative_scale(B):
+    c = Case(B, "bf16", None, 64, 16, 2, (500,), (9,), seed=27)
+    c.prob.struct.softmax_scale = -0.1
+    c.run(B.NewTokens((9,)))
+    import torch
+    out = TL.numpy64(c.out)
+    for i in (0, 8):
+        for x in (0, 15):
+            n = 500 - 9 + 1 + i
+            o, lse, _, _ = C.attend_row(c.q64[0, i, x], c.k64[0, :n, x // 8], c.v64[0, :n, x // 8], -0.1)
+            assert np.abs(out[0, i, x] - o).max() < 0.01 and abs(float(c.lse[0, x, i]) - lse) < 1e-3
