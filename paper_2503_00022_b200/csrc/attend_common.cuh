@@ -11,6 +11,8 @@
 
 #include <cooperative_groups.h>
 
+#include <atomic>
+
 #include "cache_format.cuh"
 
 namespace kvc {
@@ -394,13 +396,55 @@ __device__ __forceinline__ void join_and_write(const AttendArgs& a, const Unit& 
 
 // ---- host: the launch ------------------------------------------------------------------------------------------
 
-// Blocks of a cluster: about one round of the blocks that the chip holds (what a block does once, some microseconds, costs as much
-// as a few hundred keys), none with fewer than a tile for each of its warps.
-inline int cluster_size(long long units, int tiles, int warps, int largest, int blocks_wanted) {
-  int n = 1;
-  while (n < largest && 2 * units * n <= blocks_wanted && tiles > n * warps) n *= 2;
-  return n;
+constexpr int kMaxDevices = 64;
+
+// How many clusters of 1 .. 16 blocks of a kernel a device runs at once (write-once cache per device; 16 are more than every
+// device grants).
+struct ClusterTable {
+  std::atomic<int> held[kMaxDevices][kMaxCluster + 1];
+  // The current device's row, after the kernel may be launched with up to `bound` bytes of dynamic shared memory; NULL where
+  // something failed.
+  template <class Kernel>
+  const std::atomic<int>* resident(Kernel kern, int threads, int bound) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return nullptr; }
+    std::atomic<int>* row = held[dev];
+    if (row[1].load(std::memory_order_acquire) > 0) return row;
+    if (allow_dynamic_smem(kern, bound) != KVCRUSH_OK) return nullptr;
+    const bool large = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+    for (int c = kMaxCluster; c >= 1; --c) {
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3(c);
+      cfg.blockDim = dim3(threads);
+      cfg.dynamicSmemBytes = bound;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = c; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+      cfg.attrs = at;
+      cfg.numAttrs = 1;
+      int n = 0;
+      if ((c > 8 && !large) || cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 0) n = 0;
+      if (c == 1 && n < 1) n = sm_count();
+      row[c].store(n, std::memory_order_release);
+    }
+    cudaGetLastError();                              // of what could not be asked
+    return row;
+  }
+};
+// Blocks for each of `units` units of `tiles` tiles: the fewest rounds of resident clusters times what a block takes, its tiles and
+// `fixed` tiles' worth of what it does once.
+inline int choose_cluster(const std::atomic<int>* resident, long long units, int tiles, int fixed) {
+  int best = 1;
+  long long best_cost = -1;
+  for (int c = 1; c <= kMaxCluster && (c == 1 || 2 * c <= tiles); ++c) {
+    const int n = resident[c].load(std::memory_order_relaxed);
+    if (n < 1) continue;
+    const long long cost = (units + n - 1) / n * ((tiles + c - 1) / c + fixed);
+    if (best_cost < 0 || cost < best_cost) { best = c; best_cost = cost; }
+  }
+  return best;
 }
+
 // The grid of clusters of n_blk blocks; false: too large.
 inline bool attend_grid(const AttendArgs& a, int rows_per_block, int n_blk, dim3* grid) {
   const bool pages = a.pages.page_size > 0;

@@ -12,8 +12,6 @@
 // maximum of their own (below), since the largest weight need not belong to the largest product of weight and scale.
 #pragma once
 
-#include <atomic>
-
 #include "attend_common.cuh"
 
 namespace kvc {
@@ -21,7 +19,6 @@ namespace att {
 
 using namespace fmt;
 
-constexpr int kMaxDevices = 64;
 
 // ---- registers of a tile -----------------------------------------------------------------------------------
 
@@ -859,39 +856,6 @@ attend_kernel(AttendArgs a) {
 
 // ---- host -----------------------------------------------------------------------------------------------------
 
-// Lets the kernel be launched with up to `bound` bytes of dynamic shared memory and returns the largest cluster of it that the
-// device runs, 0 where something failed (write-once cache per device; asking costs a call 1 us): 16 blocks are more than every
-// device grants.
-template <class Kernel>
-int largest_cluster(Kernel kern, int threads, int bound, std::atomic<int>* known) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 0; }
-  const bool cached = dev >= 0 && dev < kMaxDevices;
-  if (cached) {
-    const int n = known[dev].load(std::memory_order_relaxed);
-    if (n > 0) return n;
-  }
-  if (allow_dynamic_smem(kern, bound) != KVCRUSH_OK) return 0;
-  int n = 8;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(kMaxCluster);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = bound;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = kMaxCluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  int resident = 0;
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-      cudaOccupancyMaxActiveClusters(&resident, kern, &cfg) == cudaSuccess && resident > 0)
-    n = kMaxCluster;
-  else
-    cudaGetLastError();
-  if (cached) known[dev].store(n, std::memory_order_relaxed);
-  return n;
-}
-
 template <int F, int FQ, int DP, int NB, bool kPages>
 int launch_one(AttendArgs& a, cudaStream_t stream) {
   // Two blocks an SM: a chip has room for 14 clusters of 16 then, with one only for 7.
@@ -902,10 +866,11 @@ int launch_one(AttendArgs& a, cudaStream_t stream) {
   constexpr int most = (M::kEnd + 15) / 16 * 16;
   const size_t dyn = most + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
   constexpr int bound = most + (kPages ? kMaxPagesPerSeq * 12 + 256 * 16 + 2048 : 0);
-  static std::atomic<int> known[kMaxDevices];
-  const int largest = largest_cluster(kern, kWarps * 32, bound, known);
-  if (largest == 0) return KVCRUSH_ERR_CUDA;
-  const int n_blk = cluster_size(attend_units(a, M::kRows), attend_tiles(a), kWarps, largest, 2 * sm_count());
+  static ClusterTable table;
+  const std::atomic<int>* resident = table.resident(kern, kWarps * 32, bound);
+  if (!resident) return KVCRUSH_ERR_CUDA;
+  // what a block does once takes as long as about three tiles of each of its warps
+  const int n_blk = choose_cluster(resident, attend_units(a, M::kRows), attend_tiles(a), 3 * kWarps);
   dim3 grid;
   if (!attend_grid(a, M::kRows, n_blk, &grid)) return KVCRUSH_ERR_UNSUPPORTED;
   return launch_chained(kern, grid, dim3(kWarps * 32), dyn, stream, n_blk, a);

@@ -250,11 +250,13 @@ template <int FQ, int F, bool kPages>
 int launch_one(AttendArgs& a, cudaStream_t stream) {
   auto kern = attend_simt_kernel<FQ, F, kPages>;
   const Shape& s = a.s;
-  const int n_blk = cluster_size(attend_units(a, kRows), attend_tiles(a), kWarps, 8, 4 * sm_count());
+  const size_t dyn = kOBytes + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
+  static ClusterTable table;
+  const std::atomic<int>* resident = table.resident(kern, kWarps * 32, kOBytes + (kPages ? (int)page_mem_bytes(kMaxPagesPerSeq, kMaxPagesPerSeq, kMaxD) : 0));
+  if (!resident) return KVCRUSH_ERR_CUDA;
+  const int n_blk = choose_cluster(resident, attend_units(a, kRows), attend_tiles(a), 2 * kWarps);
   dim3 grid;
   if (!attend_grid(a, kRows, n_blk, &grid)) return KVCRUSH_ERR_UNSUPPORTED;
-  const size_t dyn = kOBytes + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
-  if (allow_dynamic_smem(kern, kOBytes + (kPages ? (int)page_mem_bytes(kMaxPagesPerSeq, kMaxPagesPerSeq, kMaxD) : 0)) != KVCRUSH_OK) return KVCRUSH_ERR_CUDA;
   return launch_chained(kern, grid, dim3(kWarps * 32), dyn, stream, n_blk, a);
 }
 

@@ -8,9 +8,10 @@
 // values come by TMA; S is double-buffered (P takes the first half of its own S), so that the product of the next tile runs
 // while this one's softmax does, and two blocks share an SM.  Weights may exceed 1: the reference of a row moves only where
 // a logit is 2^8 above it, and only then the output in TMEM is scaled.
-// Whole tiles that every row sees go this way.  What is left - the tail of the cache, rows of the cache that only later
-// tokens see, and the new tokens with their mask - is a few keys for each block of the cluster, which the threads of the rows
-// add one key at a time, so that keys that a row does not see have no influence whatever they hold.
+// Tiles with keys that not every row sees (the tail of the cache, rows that only later tokens see, the new tokens with their
+// mask) come last.  A weight of 0 would take a value that is not finite along, so two helper warps look at the values of such
+// a tile first: rows that do not exist or hold a value that is not finite are cleared, and in the second case the whole tile
+// gets weight 0 and the threads of the rows add its keys one by one at the end.
 // Tree of 63 tokens x 4 heads over 32768 rows x 8 KV heads of 128: see the figures at launch_attend_tree.
 #include "attend_common.cuh"
 #include "tc_ptx.cuh"
@@ -25,7 +26,6 @@ using namespace fmt;
 constexpr int kRows = 128;                   // query rows of a block
 constexpr int kKeys = 64;                    // keys of a tile
 constexpr int kThreads = 256;                // producer, issuer, two helpers, four softmax warps
-constexpr int kTreeCluster = 8;
 constexpr int kExtra = 8;                    // keys added at a time by the rows' threads
 constexpr float kSlackLog2 = 8.f;
 constexpr uint32_t kPolls = tc::kWaitPolls;
@@ -39,15 +39,16 @@ struct TreeMem {
   static constexpr int kRing = kQ + kQBytes;
   static constexpr int kRecvO = kRing;                                  // outputs of the peers, when the ring is done with
   static constexpr int kRecvPart = kRing + 2 * kStages * kTileBytes + 256;
-  static constexpr int kAux = kRecvPart + kTreeCluster * kRows * 8;
+  static constexpr int kAux = kRecvPart + kMaxCluster * kRows * 8;
   static constexpr int kEnd = kAux + 256;
-  static_assert(kRows * DP * 4 + kTreeCluster * 16 <= 2 * kStages * kTileBytes + 256, "room for the peers' outputs");
-  static_assert(kEnd <= 112 * 1024, "two blocks an SM");
+  static_assert(kRows * DP * 4 + kMaxCluster * 16 <= 2 * kStages * kTileBytes + 256, "room for the peers' outputs");
+  static_assert(kEnd <= 113 * 1024, "two blocks an SM");
 };
 struct TreeAux {
-  unsigned long long k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_ready[2], o_done, drain;
+  // masked tiles have barriers of their own, since the helper warps do not follow the phases of the others
+  unsigned long long k_full[4], k_empty[4], v_full[4], v_empty[4], masked_full[4], v_checked[4], s_full[2], p_ready[2], o_done, drain;
   uint32_t tmem;
-  int abort_flag;
+  int abort_flag, slow;                      // slow: bit i, masked tile i of this block is added key by key
 };
 static_assert(sizeof(TreeAux) <= 256, "auxiliary memory");
 
@@ -87,7 +88,8 @@ __device__ __forceinline__ void widen8(const uint4& v, float (&x)[8]) {
 
 template <int FQ, int DP>
 __global__ void __launch_bounds__(kThreads, 2)
-attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, AttendArgs a) {
+attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_kn,
+                   const __grid_constant__ CUtensorMap map_vn, AttendArgs a) {
   using M = TreeMem<DP>;
   using tc::mbar_wait;
   extern __shared__ __align__(1024) unsigned char sh[];
@@ -105,11 +107,13 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     for (int i = 0; i < M::kStages; ++i) {
       tc::mbar_init(tc::smem_u32(&aux->k_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->k_empty[i]), 1);
       tc::mbar_init(tc::smem_u32(&aux->v_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->v_empty[i]), 1);
+      tc::mbar_init(tc::smem_u32(&aux->masked_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->v_checked[i]), 64);
     }
     for (int i = 0; i < 2; ++i) { tc::mbar_init(tc::smem_u32(&aux->s_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->p_ready[i]), kRows); }
     tc::mbar_init(tc::smem_u32(&aux->o_done), 1);
     tc::mbar_init(tc::smem_u32(&aux->drain), 1);
     aux->abort_flag = 0;
+    aux->slow = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -133,35 +137,40 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   const uint32_t tmem = aux->tmem, tmem_o = tmem + 128;
 
   const int full = (w.own ? w.seen : w.limit(0)) / kKeys;             // tiles that every row sees
-  const int per = (full + n_blk - 1) / n_blk, lo = min(full, rank * per), n = min(full, lo + per) - lo;
-  const int tail = w.seen - full * kKeys, extra = tail + w.own;       // keys that are added one by one
-  const int per_extra = (extra + n_blk - 1) / n_blk, e_lo = min(extra, rank * per_extra), e_hi = min(extra, e_lo + per_extra);
+  const int cached = (w.seen + kKeys - 1) / kKeys, total_tiles = cached + (w.own + kKeys - 1) / kKeys;
+  const int per = (total_tiles + n_blk - 1) / n_blk, lo = min(total_tiles, rank * per), n = min(total_tiles, lo + per) - lo;
+  const int n_full = max(0, min(n, full - lo));                       // of this block's tiles, those come first
+  // keys of tile t of this block that exist
+  auto keys_of = [&](int t) { return lo + t < cached ? min(kKeys, w.seen - (lo + t) * kKeys) : min(kKeys, w.own - (lo + t - cached) * kKeys); };
   float m = -FLT_MAX, l = 0.f;
-  bool has_o = n > 0;
+  const bool has_o = n > 0;
 
   if (warp == 0) {
     int issued = 0;
     if (lane == 0) {
       for (; issued < n; ++issued) {
         const int st = issued % M::kStages, round = issued / M::kStages;
-        const int row = w.begin + (lo + issued) * kKeys;
-        const uint32_t kb = tc::smem_u32(&aux->k_full[st]), vb = tc::smem_u32(&aux->v_full[st]);
+        const bool is_new = lo + issued >= cached;
+        const int row = is_new ? w.first + (lo + issued - cached) * kKeys : w.begin + (lo + issued) * kKeys;
+        const uint32_t kb = tc::smem_u32(&aux->k_full[st]), vb = tc::smem_u32(issued < n_full ? &aux->v_full[st] : &aux->masked_full[st]);
         const uint32_t kd = base + M::kRing + st * 2 * M::kTileBytes, vd = kd + M::kTileBytes;
         if (round > 0 && !mbar_wait(tc::smem_u32(&aux->k_empty[st]), (round - 1) & 1, abort_flag, kPolls)) break;
         tc::mbar_expect_tx(kb, M::kTileBytes);
-        for (int b = 0; b < M::kBlocks; ++b) tc::tma_load_4d(kd + b * kKeys * 128, &map_k, kb, b * 64, row, w.hk, w.layer);
+        for (int b = 0; b < M::kBlocks; ++b) tc::tma_load_4d(kd + b * kKeys * 128, is_new ? &map_kn : &map_k, kb, b * 64, row, w.hk, w.layer);
         if (round > 0 && !mbar_wait(tc::smem_u32(&aux->v_empty[st]), (round - 1) & 1, abort_flag, kPolls)) {
           for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(kb, round & 1); ++i) {}
           break;
         }
         tc::mbar_expect_tx(vb, M::kTileBytes);
-        for (int b = 0; b < M::kBlocks; ++b) tc::tma_load_4d(vd + b * kKeys * 128, &map_v, vb, b * 64, row, w.hk, w.layer);
+        for (int b = 0; b < M::kBlocks; ++b) tc::tma_load_4d(vd + b * kKeys * 128, is_new ? &map_vn : &map_v, vb, b * 64, row, w.hk, w.layer);
       }
       // nothing may be in flight when the block goes on: the last round's copies have landed (at once, but after a wait ran out)
       for (int t = max(0, issued - M::kStages); t < issued; ++t) {
         const int st = t % M::kStages, parity = (t / M::kStages) & 1;
         for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(tc::smem_u32(&aux->k_full[st]), parity); ++i) {}
-        for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(tc::smem_u32(&aux->v_full[st]), parity); ++i) {}
+        const uint32_t vb = tc::smem_u32(t < n_full ? &aux->v_full[st] : &aux->masked_full[st]);
+        const int v_parity = t < n_full ? parity : ((t - n_full) / M::kStages) & 1;
+        for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(vb, v_parity); ++i) {}
       }
     }
     __syncwarp();
@@ -186,7 +195,8 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       };
       auto product_o = [&](int t) {
         const int st = t % M::kStages;
-        if (!mbar_wait(tc::smem_u32(&aux->v_full[st]), (t / M::kStages) & 1, abort_flag, kPolls)) return false;
+        if (t < n_full && !mbar_wait(tc::smem_u32(&aux->v_full[st]), (t / M::kStages) & 1, abort_flag, kPolls)) return false;
+        // (the weights of a masked tile come after its values)
         if (!mbar_wait(tc::smem_u32(&aux->p_ready[t & 1]), (t >> 1) & 1, abort_flag, kPolls)) return false;
         tc::tc_fence_after();
         const uint32_t vd = base + M::kRing + st * 2 * M::kTileBytes + M::kTileBytes;
@@ -205,10 +215,58 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(tc::smem_u32(&aux->drain), 0); ++i) {}
     }
     __syncwarp();
-  } else if (warp >= 4) {
+  } else if (warp < 4) {
+    // values of the masked tiles
+    const int h = tid - 64;
+    for (int t = n_full; t < n; ++t) {
+      const int st = t % M::kStages, keys = keys_of(t);
+      if (!__all_sync(kAll, mbar_wait(tc::smem_u32(&aux->masked_full[st]), ((t - n_full) / M::kStages) & 1, abort_flag, kPolls))) break;
+      unsigned char* vd = sh + M::kRing + st * 2 * M::kTileBytes + M::kTileBytes + h * 128;      // row h of every block of channels
+      bool bad = false;
+      if (h < keys)
+        for (int b = 0; b < M::kBlocks; ++b)
+          for (int c = 0; c < 8; ++c) {
+            const uint4 v = *reinterpret_cast<const uint4*>(vd + b * kKeys * 128 + c * 16);
+            const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              constexpr uint32_t e = FQ == KVCRUSH_BF16 ? 0x7F80u : 0x7C00u;
+              bad |= (x[i] & e) == e || (x[i] >> 16 & e) == e;
+            }
+          }
+      if (bad) atomicOr(&aux->slow, 1 << (t - n_full));                // the whole tile then has weight 0, in its other rows too
+      if (h >= keys || bad)
+        for (int b = 0; b < M::kBlocks; ++b)
+          for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vd + b * kKeys * 128 + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+      proxy_fence();
+      tc::mbar_arrive(tc::smem_u32(&aux->v_checked[st]));
+    }
+  } else {
     const uint32_t lanes = (uint32_t)(warp - 4) * 32u << 16;
     const int r = (warp - 4) * 32 + lane;
     const float scale = a.scale_log2;
+    const int tok = w.token(min(r, w.rows - 1)), limit = w.limit(min(r, w.rows - 1));
+    // which keys of masked tile t this row sees
+    auto seen_of = [&](int t) {
+      const int keys = keys_of(t);
+      unsigned long long see = keys >= 64 ? ~0ull : (1ull << keys) - 1ull;
+      if (lo + t < cached) {
+        const int left = max(0, limit - (lo + t) * kKeys);
+        if (left < 64) see &= (1ull << left) - 1ull;
+      } else {
+        const int first = (lo + t - cached) * kKeys;
+        if (!a.fresh.mask) {
+          const int left = max(0, tok + 1 - first);
+          if (left < 64) see &= (1ull << left) - 1ull;
+        } else {
+          const uint32_t* row = a.fresh.mask + (long long)(w.first + tok) * a.fresh.mask_words + first / 32;
+          unsigned long long bits = __ldg(row);
+          if (first / 32 + 1 < a.fresh.mask_words) bits |= (unsigned long long)__ldg(row + 1) << 32;
+          see &= bits;
+        }
+      }
+      return see;
+    };
     bool ok = true;
     auto wait = [&](unsigned long long* bar, int parity) {             // one answer for the warp
       return (bool)__all_sync(kAll, mbar_wait(tc::smem_u32(bar), parity, abort_flag, kPolls));
@@ -235,6 +293,12 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       for (int i = 0; i < 4; ++i) tc::tmem_ld16(at + 16 * i, v[i]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) tc::tmem_wait16(v[i]);
+      if (t >= n_full) {
+        if (!wait(&aux->v_checked[t % M::kStages], ((t - n_full) / M::kStages) & 1)) { ok = false; break; }
+        const unsigned long long see = *reinterpret_cast<volatile int*>(&aux->slow) >> (t - n_full) & 1 ? 0ull : seen_of(t);
+#pragma unroll
+        for (int i = 0; i < 64; ++i) v[i >> 4][i & 15] = see >> i & 1ull ? v[i >> 4][i & 15] : 0xFF800000u;
+      }
       float top[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -278,31 +342,29 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (ok && n > 0) ok = wait(&aux->o_done, (n - 1) & 1);
     tc::tc_fence_after();
     // keys that are added one by one
-    if (ok) {
-      const int tok = w.token(min(r, w.rows - 1)), limit = w.limit(min(r, w.rows - 1));
-      const unsigned char* kc = static_cast<const unsigned char*>(a.K.ptr) + bytes_of<FQ>(w.layer * a.K.sl + w.hk * a.K.sh);
-      const unsigned char* vc = static_cast<const unsigned char*>(a.V.ptr) + bytes_of<FQ>(w.layer * a.V.sl + w.hk * a.V.sh);
-      const unsigned char* kn = static_cast<const unsigned char*>(a.K_new.ptr) + bytes_of<FQ>(w.layer * a.K_new.sl + w.hk * a.K_new.sh);
-      const unsigned char* vn = static_cast<const unsigned char*>(a.V_new.ptr) + bytes_of<FQ>(w.layer * a.V_new.sl + w.hk * a.V_new.sh);
+    const int slow = ok ? *reinterpret_cast<volatile int*>(&aux->slow) : 0;
 #pragma unroll 1
-      for (int e0 = e_lo; e0 < e_hi; e0 += kExtra) {
+    for (int t = n_full; t < n; ++t) {
+      if (!(slow >> (t - n_full) & 1)) continue;
+      const unsigned long long see = seen_of(t);
+      const bool is_new = lo + t >= cached;
+      const TensorView kv{a.K.ptr, a.K.dtype, a.K.sl, a.K.st, a.K.sh}, vv{a.V.ptr, a.V.dtype, a.V.sl, a.V.st, a.V.sh};
+      const TensorView ks = is_new ? a.K_new : kv, vs = is_new ? a.V_new : vv;
+      const long long row0 = is_new ? w.first + (lo + t - cached) * kKeys : w.begin + (lo + t) * kKeys;
+      const unsigned char* kb = static_cast<const unsigned char*>(ks.ptr) + bytes_of<FQ>(w.layer * ks.sl + w.hk * ks.sh + row0 * ks.st);
+      const unsigned char* vb = static_cast<const unsigned char*>(vs.ptr) + bytes_of<FQ>(w.layer * vs.sl + w.hk * vs.sh + row0 * vs.st);
+      const int keys = keys_of(t);
+#pragma unroll 1
+      for (int e0 = 0; e0 < keys; e0 += kExtra) {
         const unsigned char *kp[kExtra], *vp[kExtra];
         float x[kExtra];
         bool sees[kExtra];
         float most = -FLT_MAX;
 #pragma unroll
         for (int j = 0; j < kExtra; ++j) {
-          const int e = min(e0 + j, e_hi - 1);
-          if (e < tail) {
-            const long long row = w.begin + full * kKeys + e;
-            kp[j] = kc + bytes_of<FQ>(row * a.K.st); vp[j] = vc + bytes_of<FQ>(row * a.V.st);
-            sees[j] = full * kKeys + e < limit;
-          } else {
-            const long long row = w.first + e - tail;
-            kp[j] = kn + bytes_of<FQ>(row * a.K_new.st); vp[j] = vn + bytes_of<FQ>(row * a.V_new.st);
-            sees[j] = sees_new(a, w, tok, e - tail);
-          }
-          sees[j] = sees[j] && e0 + j < e_hi;
+          const int e = min(e0 + j, keys - 1);
+          kp[j] = kb + bytes_of<FQ>(e * ks.st); vp[j] = vb + bytes_of<FQ>(e * vs.st);
+          sees[j] = e0 + j < keys && (see >> e & 1ull);
           x[j] = 0.f;
         }
 #pragma unroll 1
@@ -333,12 +395,10 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll 1
         for (int c = 0; c < DP; c += 16) {
           uint32_t o[16];
-          if (has_o) {
-            tc::tmem_ld16(tmem_o + lanes + c, o);
-            tc::tmem_wait16(o);
-          }
+          tc::tmem_ld16(tmem_o + lanes + c, o);
+          tc::tmem_wait16(o);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = has_o ? __float_as_uint(__uint_as_float(o[i]) * f) : 0u;
+          for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (c + 8 * h >= s.D) break;
@@ -355,7 +415,6 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           tmem_st16(tmem_o + lanes + c, o);
         }
         tmem_wait_st();
-        has_o = true;
       }
     }
   }
@@ -374,7 +433,6 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         float2* dst = recv_part + rank * kRows + r;
         *(n_blk > 1 ? cluster.map_shared_rank(dst, p) : dst) = make_float2(m, l);
       }
-    has_o = __any_sync(kAll, has_o);
 #pragma unroll 1
     for (int c = 0; c < DP; c += 16) {
       uint32_t o[16];
@@ -426,15 +484,17 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 }
 
 template <int FQ, int DP>
-int launch_one(const AttendArgs& a, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
+int launch_one(const AttendArgs& a, const CUtensorMap (&maps)[4], cudaStream_t stream) {
   using M = TreeMem<DP>;
   auto kern = attend_tree_kernel<FQ, DP>;
-  if (allow_dynamic_smem(kern, M::kEnd) != KVCRUSH_OK) return KVCRUSH_ERR_CUDA;
-  const int tiles = (a.s.max_seqlen + kKeys - 1) / kKeys;
-  const int n_blk = cluster_size(attend_units(a, kRows), tiles, 2, kTreeCluster, 2 * sm_count());
+  static ClusterTable table;
+  const std::atomic<int>* resident = table.resident(kern, kThreads, M::kEnd);
+  if (!resident) return KVCRUSH_ERR_CUDA;
+  // what a block does once takes as long as about five tiles
+  const int n_blk = choose_cluster(resident, attend_units(a, kRows), (a.s.max_seqlen + (a.K_new.ptr ? a.fresh.most : 0) + kKeys - 1) / kKeys, 5);
   dim3 grid;
   if (!attend_grid(a, kRows, n_blk, &grid)) return KVCRUSH_ERR_UNSUPPORTED;
-  return launch_chained(kern, grid, dim3(kThreads), M::kEnd, stream, n_blk, mk, mv, a);
+  return launch_chained(kern, grid, dim3(kThreads), M::kEnd, stream, n_blk, maps[0], maps[1], maps[2], maps[3], a);
 }
 
 }  // namespace
@@ -446,12 +506,17 @@ bool attend_tree_fits(const AttendArgs& a) {
 }
 
 int launch_attend_tree(const AttendArgs& a, bool* taken, cudaStream_t stream) {
-  CUtensorMap mk, mv;
-  const TensorView k{a.K.ptr, a.K.dtype, a.K.sl, a.K.st, a.K.sh}, v{a.V.ptr, a.V.dtype, a.V.sl, a.V.st, a.V.sh};
-  *taken = a.s.T > 0 && tc::make_map(&mk, k, a.s.D, a.s.T, a.s.Hkv, a.s.n_layers, kKeys) && tc::make_map(&mv, v, a.s.D, a.s.T, a.s.Hkv, a.s.n_layers, kKeys);
+  CUtensorMap maps[4];
+  const TensorView cache[2] = {{a.K.ptr, a.K.dtype, a.K.sl, a.K.st, a.K.sh}, {a.V.ptr, a.V.dtype, a.V.sl, a.V.st, a.V.sh}};
+  *taken = a.s.T > 0;
+  for (int i = 0; i < 2 && *taken; ++i) {
+    *taken = tc::make_map(&maps[i], cache[i], a.s.D, a.s.T, a.s.Hkv, a.s.n_layers, kKeys);
+    if (*taken && a.K_new.ptr) *taken = tc::make_map(&maps[2 + i], i ? a.V_new : a.K_new, a.s.D, a.fresh.total, a.s.Hkv, a.s.n_layers, kKeys);
+    else maps[2 + i] = maps[i];
+  }
   if (!*taken) return KVCRUSH_OK;
-  if (a.K.dtype == KVCRUSH_BF16) return a.s.D <= 64 ? launch_one<KVCRUSH_BF16, 64>(a, mk, mv, stream) : launch_one<KVCRUSH_BF16, 128>(a, mk, mv, stream);
-  return a.s.D <= 64 ? launch_one<KVCRUSH_FP16, 64>(a, mk, mv, stream) : launch_one<KVCRUSH_FP16, 128>(a, mk, mv, stream);
+  if (a.K.dtype == KVCRUSH_BF16) return a.s.D <= 64 ? launch_one<KVCRUSH_BF16, 64>(a, maps, stream) : launch_one<KVCRUSH_BF16, 128>(a, maps, stream);
+  return a.s.D <= 64 ? launch_one<KVCRUSH_FP16, 64>(a, maps, stream) : launch_one<KVCRUSH_FP16, 128>(a, maps, stream);
 }
 
 }  // namespace kvc
