@@ -5,11 +5,12 @@
 // work.  A block takes 128 query rows (TMEM lane = row) of one (layer, sequence, KV head) and a share of the keys, in tiles of
 // 64: S = Q K^T, the softmax in registers of the thread that owns the row, P back to TMEM as the left operand of O += P V, whose
 // right operand V is read as it lies in memory (its channels are the fast axis).  The queries stay in shared memory, keys and
-// values come by TMA; S is double-buffered (P takes the first half of its own S), so that the product of the next tile runs
-// while this one's softmax does, and two blocks share an SM.  Weights may exceed 1: the reference of a row moves only where
-// a logit is 2^8 above it, and only then the output in TMEM is scaled.
+// values come by TMA into a ring.  Even and odd tiles are two streams with a softmax warpgroup, an output and two buffers of S
+// each (P takes the first half of its own S; 512 columns in all), so that one stream's products and waits pass while the other
+// takes its exponentials, which bound the kernel (16 a clock and SM).  Weights may exceed 1: the reference of a row moves only
+// where a logit is 2^8 above it, and only then the output in TMEM is scaled.
 // Tiles with keys that not every row sees (the tail of the cache, rows that only later tokens see, the new tokens with their
-// mask) come last.  A weight of 0 would take a value that is not finite along, so two helper warps look at the values of such
+// mask) come last.  A weight of 0 would take a value that is not finite along, so a helper warp looks at the values of such
 // a tile first: rows that do not exist or hold a value that is not finite are cleared, and in the second case the whole tile
 // gets weight 0 and the threads of the rows add its keys one by one at the end.
 // Tree of 63 tokens x 4 heads over 32768 rows x 8 KV heads of 128: see the figures at launch_attend_tree.
@@ -25,7 +26,7 @@ using namespace fmt;
 
 constexpr int kRows = 128;                   // query rows of a block
 constexpr int kKeys = 64;                    // keys of a tile
-constexpr int kThreads = 256;                // producer, issuer, two helpers, four softmax warps
+constexpr int kThreads = 384;                // producer, an issuer for each stream, helper, two softmax warpgroups
 constexpr int kExtra = 8;                    // keys added at a time by the rows' threads
 constexpr float kSlackLog2 = 8.f;
 constexpr uint32_t kPolls = tc::kWaitPolls;
@@ -33,24 +34,25 @@ constexpr uint32_t kPolls = tc::kWaitPolls;
 template <int DP>
 struct TreeMem {
   static constexpr int kBlocks = DP / 64;                               // of 64 channels: 128-byte rows
-  static constexpr int kStages = DP == 128 ? 2 : 4;
+  static constexpr int kStages = DP == 128 ? 5 : 8;
   static constexpr int kQ = 0, kQBytes = kBlocks * kRows * 128;
   static constexpr int kTileBytes = kBlocks * kKeys * 128;              // keys or values of a stage
   static constexpr int kRing = kQ + kQBytes;
   static constexpr int kRecvO = kRing;                                  // outputs of the peers, when the ring is done with
   static constexpr int kRecvPart = kRing + 2 * kStages * kTileBytes + 256;
   static constexpr int kAux = kRecvPart + kMaxCluster * kRows * 8;
-  static constexpr int kEnd = kAux + 256;
+  static constexpr int kEnd = kAux + 3072;
   static_assert(kRows * DP * 4 + kMaxCluster * 16 <= 2 * kStages * kTileBytes + 256, "room for the peers' outputs");
-  static_assert(kEnd <= 113 * 1024, "two blocks an SM");
+  static_assert(kEnd <= 227 * 1024, "one block an SM");
 };
 struct TreeAux {
-  // masked tiles have barriers of their own, since the helper warps do not follow the phases of the others
-  unsigned long long k_full[4], k_empty[4], v_full[4], v_empty[4], masked_full[4], v_checked[4], s_full[2], p_ready[2], o_done, drain;
+  // masked tiles have barriers of their own, since the helper warp does not follow the phases of the others
+  unsigned long long k_full[8], k_empty[8], v_full[8], v_empty[8], masked_full[8], v_checked[8], s_full[2][2], p_ready[2][2], o_done[2], drain;
+  float2 stats[2][kRows];                    // of the two streams, at the end
   uint32_t tmem;
   int abort_flag, slow;                      // slow: bit i, masked tile i of this block is added key by key
 };
-static_assert(sizeof(TreeAux) <= 256, "auxiliary memory");
+static_assert(sizeof(TreeAux) <= 3072, "auxiliary memory");
 
 // Descriptor of 16 keys x 64 or 128 channels of values: rows of 64 channels (128 bytes, 128-byte swizzle), eight keys 1024 bytes
 // apart, blocks of 64 channels kKeys rows apart.
@@ -76,6 +78,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// One lane of the warp, the same each time; the code around stays uniform, so that descriptors are made in uniform registers
+// (a thread by itself took 75 cycles for each product it issued).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+  return ok != 0;
+}
+
 template <int FQ>
 __device__ __forceinline__ void widen8(const uint4& v, float (&x)[8]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -87,7 +97,7 @@ __device__ __forceinline__ void widen8(const uint4& v, float (&x)[8]) {
 }
 
 template <int FQ, int DP>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, 1)
 attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_kn,
                    const __grid_constant__ CUtensorMap map_vn, AttendArgs a) {
   using M = TreeMem<DP>;
@@ -107,17 +117,19 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     for (int i = 0; i < M::kStages; ++i) {
       tc::mbar_init(tc::smem_u32(&aux->k_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->k_empty[i]), 1);
       tc::mbar_init(tc::smem_u32(&aux->v_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->v_empty[i]), 1);
-      tc::mbar_init(tc::smem_u32(&aux->masked_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->v_checked[i]), 64);
+      tc::mbar_init(tc::smem_u32(&aux->masked_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->v_checked[i]), 32);
     }
-    for (int i = 0; i < 2; ++i) { tc::mbar_init(tc::smem_u32(&aux->s_full[i]), 1); tc::mbar_init(tc::smem_u32(&aux->p_ready[i]), kRows); }
-    tc::mbar_init(tc::smem_u32(&aux->o_done), 1);
-    tc::mbar_init(tc::smem_u32(&aux->drain), 1);
+    for (int x = 0; x < 2; ++x) {
+      for (int i = 0; i < 2; ++i) { tc::mbar_init(tc::smem_u32(&aux->s_full[x][i]), 1); tc::mbar_init(tc::smem_u32(&aux->p_ready[x][i]), kRows); }
+      tc::mbar_init(tc::smem_u32(&aux->o_done[x]), 1);
+    }
+    tc::mbar_init(tc::smem_u32(&aux->drain), 2);
     aux->abort_flag = 0;
     aux->slow = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    tc::tmem_alloc(tc::smem_u32(&aux->tmem), 256);
+    tc::tmem_alloc(tc::smem_u32(&aux->tmem), 512);
     tc::tmem_relinquish();
   }
   // queries: rows of 128 bytes, 128-byte swizzle, as TMA would lay them out
@@ -134,7 +146,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   __syncthreads();
   tc::tc_fence_after();
   volatile int* abort_flag = &aux->abort_flag;
-  const uint32_t tmem = aux->tmem, tmem_o = tmem + 128;
+  const uint32_t tmem = aux->tmem;                                    // stream x: S in columns 256 x, 256 x + 64, O from 256 x + 128 on
 
   const int full = (w.own ? w.seen : w.limit(0)) / kKeys;             // tiles that every row sees
   const int cached = (w.seen + kKeys - 1) / kKeys, total_tiles = cached + (w.own + kKeys - 1) / kKeys;
@@ -142,8 +154,6 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   const int n_full = max(0, min(n, full - lo));                       // of this block's tiles, those come first
   // keys of tile t of this block that exist
   auto keys_of = [&](int t) { return lo + t < cached ? min(kKeys, w.seen - (lo + t) * kKeys) : min(kKeys, w.own - (lo + t - cached) * kKeys); };
-  float m = -FLT_MAX, l = 0.f;
-  const bool has_o = n > 0;
 
   if (warp == 0) {
     int issued = 0;
@@ -174,77 +184,103 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
     }
     __syncwarp();
-  } else if (warp == 1) {
-    if (lane == 0 && n > 0) {
+  } else if (warp < 3) {
+    // one issuer for each stream: a single one is bound by what it does between products (1800 cycles a tile)
+    const int x = warp - 1;
+    if (n > 0) {                                       // the whole warp follows, one lane issues
       constexpr uint32_t idesc_s = tc::make_idesc(kRows, kKeys, FQ == KVCRUSH_BF16);
       constexpr uint32_t idesc_o = tc::make_idesc(kRows, DP, FQ == KVCRUSH_BF16) | 1u << 16;      // right operand: channels are the fast axis
-      auto product_s = [&](int t) {
-        const int st = t % M::kStages;
-        // S takes the place of the weights of two tiles before, which that tile's product has read
-        if (t >= 2 && !mbar_wait(tc::smem_u32(&aux->o_done), t & 1, abort_flag, kPolls)) return false;
-        if (!mbar_wait(tc::smem_u32(&aux->k_full[st]), (t / M::kStages) & 1, abort_flag, kPolls)) return false;
+      const uint64_t desc_q = tc::smem_desc_sw128(base + M::kQ), desc_k = tc::smem_desc_sw128(base + M::kRing);
+      const uint64_t desc_v = values_desc(base + M::kRing + M::kTileBytes);
+      auto wait = [&](unsigned long long* bar, int parity) {
+        return (bool)__all_sync(kAll, mbar_wait(tc::smem_u32(bar), parity, abort_flag, kPolls));
+      };
+      auto product_s = [&](int t, int st, int parity) {
+        const int u = t >> 1;
+        // S takes the place of the weights of two tiles before in its stream, which that tile's product has read
+        if (u >= 2 && !wait(&aux->o_done[x], u & 1)) return false;
+        if (!wait(&aux->k_full[st], parity)) return false;
         tc::tc_fence_after();
-        const uint32_t kd = base + M::kRing + st * 2 * M::kTileBytes;
+        const uint32_t d = tmem + x * 256 + (u & 1) * kKeys;
+        const uint64_t dk = desc_k + (uint32_t)(st * (2 * M::kTileBytes >> 4));
+        if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-          tc::umma_bf16(tmem + (t & 1) * kKeys, tc::smem_desc_sw128(base + M::kQ + (k >> 2) * kRows * 128 + (k & 3) * 32),
-                        tc::smem_desc_sw128(kd + (k >> 2) * kKeys * 128 + (k & 3) * 32), idesc_s, k > 0);
-        tc::umma_commit(tc::smem_u32(&aux->k_empty[st]));
-        tc::umma_commit(tc::smem_u32(&aux->s_full[t & 1]));
+          for (int k = 0; k < DP / 16; ++k)
+            tc::umma_bf16(d, desc_q + ((k >> 2) * kRows * 128 + (k & 3) * 32 >> 4), dk + ((k >> 2) * kKeys * 128 + (k & 3) * 32 >> 4), idesc_s, k > 0);
+          tc::umma_commit(tc::smem_u32(&aux->k_empty[st]));
+          tc::umma_commit(tc::smem_u32(&aux->s_full[x][u & 1]));
+        }
+        __syncwarp();
         return true;
       };
-      auto product_o = [&](int t) {
-        const int st = t % M::kStages;
-        if (t < n_full && !mbar_wait(tc::smem_u32(&aux->v_full[st]), (t / M::kStages) & 1, abort_flag, kPolls)) return false;
+      auto product_o = [&](int t, int st, int parity) {
+        const int u = t >> 1;
+        if (t < n_full && !wait(&aux->v_full[st], parity)) return false;
         // (the weights of a masked tile come after its values)
-        if (!mbar_wait(tc::smem_u32(&aux->p_ready[t & 1]), (t >> 1) & 1, abort_flag, kPolls)) return false;
+        if (!wait(&aux->p_ready[x][u & 1], (u >> 1) & 1)) return false;
         tc::tc_fence_after();
-        const uint32_t vd = base + M::kRing + st * 2 * M::kTileBytes + M::kTileBytes;
+        const uint32_t d = tmem + x * 256 + 128, p = tmem + x * 256 + (u & 1) * kKeys;
+        const uint64_t dv = desc_v + (uint32_t)(st * (2 * M::kTileBytes >> 4));
+        if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < kKeys / 16; ++k)
-          umma_p(tmem_o, tmem + (t & 1) * kKeys + k * 8, values_desc(vd + k * 16 * 128), idesc_o, t > 0 || k > 0);
-        tc::umma_commit(tc::smem_u32(&aux->v_empty[st]));
-        tc::umma_commit(tc::smem_u32(&aux->o_done));
+          for (int k = 0; k < kKeys / 16; ++k) umma_p(d, p + k * 8, dv + (k * 16 * 128 >> 4), idesc_o, u > 0 || k > 0);
+          tc::umma_commit(tc::smem_u32(&aux->v_empty[st]));
+          tc::umma_commit(tc::smem_u32(&aux->o_done[x]));
+        }
+        __syncwarp();
         return true;
       };
-      bool ok = product_s(0);
-      for (int t = 1; ok && t < n; ++t) ok = product_s(t) && product_o(t - 1);
-      if (ok) product_o(n - 1);
+      bool ok = true;
+      int st = x, parity = 0, st_o = x, parity_o = 0;   // ring positions of the two products
+      for (int t = x; ok && t < n + 2; t += 2) {
+        if (t < n) {
+          ok = product_s(t, st, parity);
+          if ((st += 2) >= M::kStages) { st -= M::kStages; parity ^= 1; }
+        }
+        if (ok && t >= 2) {
+          ok = product_o(t - 2, st_o, parity_o);
+          if ((st_o += 2) >= M::kStages) { st_o -= M::kStages; parity_o ^= 1; }
+        }
+      }
       // products in flight end before TMEM is freed
-      tc::umma_commit(tc::smem_u32(&aux->drain));
+      if (elect_one()) tc::umma_commit(tc::smem_u32(&aux->drain));
+      __syncwarp();
       for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(tc::smem_u32(&aux->drain), 0); ++i) {}
     }
     __syncwarp();
   } else if (warp < 4) {
-    // values of the masked tiles
-    const int h = tid - 64;
+    // values of the masked tiles: a lane looks at rows lane and lane + 32
     for (int t = n_full; t < n; ++t) {
       const int st = t % M::kStages, keys = keys_of(t);
       if (!__all_sync(kAll, mbar_wait(tc::smem_u32(&aux->masked_full[st]), ((t - n_full) / M::kStages) & 1, abort_flag, kPolls))) break;
-      unsigned char* vd = sh + M::kRing + st * 2 * M::kTileBytes + M::kTileBytes + h * 128;      // row h of every block of channels
-      bool bad = false;
-      if (h < keys)
-        for (int b = 0; b < M::kBlocks; ++b)
-          for (int c = 0; c < 8; ++c) {
-            const uint4 v = *reinterpret_cast<const uint4*>(vd + b * kKeys * 128 + c * 16);
-            const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+      for (int h = lane; h < kKeys; h += 32) {
+        unsigned char* vd = sh + M::kRing + st * 2 * M::kTileBytes + M::kTileBytes + h * 128;    // row h of every block of channels
+        bool bad = false;
+        if (h < keys)
+          for (int b = 0; b < M::kBlocks; ++b)
+            for (int c = 0; c < 8; ++c) {
+              const uint4 v = *reinterpret_cast<const uint4*>(vd + b * kKeys * 128 + c * 16);
+              const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              constexpr uint32_t e = FQ == KVCRUSH_BF16 ? 0x7F80u : 0x7C00u;
-              bad |= (x[i] & e) == e || (x[i] >> 16 & e) == e;
+              for (int i = 0; i < 4; ++i) {
+                constexpr uint32_t e = FQ == KVCRUSH_BF16 ? 0x7F80u : 0x7C00u;
+                bad |= (x[i] & e) == e || (x[i] >> 16 & e) == e;
+              }
             }
-          }
-      if (bad) atomicOr(&aux->slow, 1 << (t - n_full));                // the whole tile then has weight 0, in its other rows too
-      if (h >= keys || bad)
-        for (int b = 0; b < M::kBlocks; ++b)
-          for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vd + b * kKeys * 128 + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+        if (bad) atomicOr(&aux->slow, 1 << (t - n_full));              // the whole tile then has weight 0, in its other rows too
+        if (h >= keys || bad)
+          for (int b = 0; b < M::kBlocks; ++b)
+            for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vd + b * kKeys * 128 + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+      }
       proxy_fence();
       tc::mbar_arrive(tc::smem_u32(&aux->v_checked[st]));
     }
   } else {
-    const uint32_t lanes = (uint32_t)(warp - 4) * 32u << 16;
-    const int r = (warp - 4) * 32 + lane;
+    const int x = (warp - 4) >> 2;                     // stream: tiles x, x + 2, ..
+    const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16, tmem_o = tmem + x * 256 + 128;
+    const int r = (warp & 3) * 32 + lane;
     const float scale = a.scale_log2;
+    float m = -FLT_MAX, l = 0.f;
     const int tok = w.token(min(r, w.rows - 1)), limit = w.limit(min(r, w.rows - 1));
     // which keys of masked tile t this row sees
     auto seen_of = [&](int t) {
@@ -284,10 +320,11 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
       tmem_wait_st();
     };
-    for (int t = 0; t < n; ++t) {
-      if (!wait(&aux->s_full[t & 1], (t >> 1) & 1)) { ok = false; break; }
+    for (int t = x; t < n; t += 2) {
+      const int u = t >> 1;
+      if (!wait(&aux->s_full[x][u & 1], (u >> 1) & 1)) { ok = false; break; }
       tc::tc_fence_after();
-      const uint32_t at = tmem + lanes + (t & 1) * kKeys;
+      const uint32_t at = tmem + x * 256 + lanes + (u & 1) * kKeys;
       uint32_t v[4][16];
 #pragma unroll
       for (int i = 0; i < 4; ++i) tc::tmem_ld16(at + 16 * i, v[i]);
@@ -312,8 +349,8 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const float m_new = fmaxf(m, most), f = ex2(m - m_new);
         m = m_new;
         l *= f;
-        if (t > 0) {                                   // the product of the tile before may still add to the output
-          if (!wait(&aux->o_done, (t - 1) & 1)) { ok = false; break; }
+        if (u > 0) {                                   // the product of the tile before may still add to the output
+          if (!wait(&aux->o_done[x], (u - 1) & 1)) { ok = false; break; }
           tc::tc_fence_after();
           scale_output(f);
         }
@@ -337,15 +374,16 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       l += tc::sum4(sum);
       tmem_wait_st();
       tc::tc_fence_before();
-      tc::mbar_arrive(tc::smem_u32(&aux->p_ready[t & 1]));
+      tc::mbar_arrive(tc::smem_u32(&aux->p_ready[x][u & 1]));
     }
-    if (ok && n > 0) ok = wait(&aux->o_done, (n - 1) & 1);
+    const int mine = (n - x + 1) >> 1;                 // tiles of this stream
+    if (ok && mine > 0) ok = wait(&aux->o_done[x], (mine - 1) & 1);
     tc::tc_fence_after();
     // keys that are added one by one
     const int slow = ok ? *reinterpret_cast<volatile int*>(&aux->slow) : 0;
 #pragma unroll 1
     for (int t = n_full; t < n; ++t) {
-      if (!(slow >> (t - n_full) & 1)) continue;
+      if ((t & 1) != x || !(slow >> (t - n_full) & 1)) continue;
       const unsigned long long see = seen_of(t);
       const bool is_new = lo + t >= cached;
       const TensorView kv{a.K.ptr, a.K.dtype, a.K.sl, a.K.st, a.K.sh}, vv{a.V.ptr, a.V.dtype, a.V.sl, a.V.st, a.V.sh};
@@ -357,7 +395,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll 1
       for (int e0 = 0; e0 < keys; e0 += kExtra) {
         const unsigned char *kp[kExtra], *vp[kExtra];
-        float x[kExtra];
+        float y[kExtra];
         bool sees[kExtra];
         float most = -FLT_MAX;
 #pragma unroll
@@ -365,7 +403,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           const int e = min(e0 + j, keys - 1);
           kp[j] = kb + bytes_of<FQ>(e * ks.st); vp[j] = vb + bytes_of<FQ>(e * vs.st);
           sees[j] = e0 + j < keys && (see >> e & 1ull);
-          x[j] = 0.f;
+          y[j] = 0.f;
         }
 #pragma unroll 1
         for (int c = 0; c < s.D / 8; ++c) {
@@ -376,21 +414,21 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             float k[8];
             widen8<FQ>(__ldg(reinterpret_cast<const uint4*>(kp[j]) + c), k);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[j] = fmaf(q[i], k[i], x[j]);
+            for (int i = 0; i < 8; ++i) y[j] = fmaf(q[i], k[i], y[j]);
           }
         }
 #pragma unroll
         for (int j = 0; j < kExtra; ++j) {
-          x[j] = sees[j] ? x[j] * scale : neg_inf();
-          most = fmaxf(most, x[j]);
+          y[j] = sees[j] ? y[j] * scale : neg_inf();
+          most = fmaxf(most, y[j]);
         }
         const float m_new = fmaxf(m, most), f = ex2(m - m_new);
         m = m_new;
         l *= f;
 #pragma unroll
         for (int j = 0; j < kExtra; ++j) {
-          x[j] = ex2(x[j] - m);
-          l += sees[j] ? x[j] : 0.f;
+          y[j] = ex2(y[j] - m);
+          l += sees[j] ? y[j] : 0.f;
         }
 #pragma unroll 1
         for (int c = 0; c < DP; c += 16) {
@@ -408,7 +446,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
               widen8<FQ>(__ldg(reinterpret_cast<const uint4*>(vp[j]) + c / 8 + h), v);
               if (sees[j]) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o[8 * h + i] = __float_as_uint(fmaf(x[j], v[i], __uint_as_float(o[8 * h + i])));
+                for (int i = 0; i < 8; ++i) o[8 * h + i] = __float_as_uint(fmaf(y[j], v[i], __uint_as_float(o[8 * h + i])));
               }
             }
           }
@@ -417,6 +455,8 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         tmem_wait_st();
       }
     }
+    aux->stats[x][r] = make_float2(m, l);
+    tc::tc_fence_before();
   }
   // The join: a row's thread sends its outputs to the owners of their shares.  The peers' rings are free when all have come here.
   __syncthreads();
@@ -426,19 +466,26 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   float2* recv_part = reinterpret_cast<float2*>(sh + M::kRecvPart);
   if (n_blk > 1) { cluster_arrive(); cluster_wait(); }
   if (warp >= 4) {
-    const uint32_t lanes = (uint32_t)(warp - 4) * 32u << 16;
-    const int r = (warp - 4) * 32 + lane;
-    if (r < w.rows)
+    // either warpgroup joins the streams in half of the channels
+    tc::tc_fence_after();
+    const int half = (warp - 4) >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t at = tmem + ((uint32_t)(warp & 3) * 32u << 16) + 128;
+    const float2 s0 = aux->stats[0][r], s1 = aux->stats[1][r];
+    const float m = fmaxf(s0.x, s1.x), f0 = ex2(s0.x - m), f1 = ex2(s1.x - m);
+    if (half == 0 && r < w.rows)
       for (int p = 0; p < n_blk; ++p) {
         float2* dst = recv_part + rank * kRows + r;
-        *(n_blk > 1 ? cluster.map_shared_rank(dst, p) : dst) = make_float2(m, l);
+        *(n_blk > 1 ? cluster.map_shared_rank(dst, p) : dst) = make_float2(m, fmaf(s0.y, f0, s1.y * f1));
       }
 #pragma unroll 1
-    for (int c = 0; c < DP; c += 16) {
-      uint32_t o[16];
-      if (has_o) {
-        tc::tmem_ld16(tmem_o + lanes + c, o);
-        tc::tmem_wait16(o);
+    for (int c = half * DP / 2; c < (half + 1) * DP / 2; c += 16) {
+      uint32_t o[16], o1[16];
+      if (n > 0) { tc::tmem_ld16(at + c, o); tc::tmem_wait16(o); }
+      if (n > 1) { tc::tmem_ld16(at + 256 + c, o1); tc::tmem_wait16(o1); }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = n > 0 ? __uint_as_float(o[i]) * f0 : 0.f;
+        o[i] = __float_as_uint(n > 1 ? fmaf(__uint_as_float(o1[i]), f1, y) : y);
       }
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
@@ -446,7 +493,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           const int e = r * vec + (c + i) / 4, owner = n_blk == 1 ? 0 : share == 1 ? e : (int)__umulhi((uint32_t)e, share_magic);
           float4* dst = recv_o + rank * share + (e - owner * share);
           *(n_blk > 1 ? cluster.map_shared_rank(dst, owner) : dst) =
-              has_o ? make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3])) : make_float4(0.f, 0.f, 0.f, 0.f);
+              make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
         }
       }
     }
@@ -455,7 +502,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   if (n_blk > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
   if (warp == 1) {
     tc::tc_fence_after();
-    tc::tmem_dealloc(tmem, 256);
+    tc::tmem_dealloc(tmem, 512);
   }
   const int mine = rank * share;
   for (int i = tid; i < min(share, total - mine); i += kThreads) {
@@ -490,8 +537,8 @@ int launch_one(const AttendArgs& a, const CUtensorMap (&maps)[4], cudaStream_t s
   static ClusterTable table;
   const std::atomic<int>* resident = table.resident(kern, kThreads, M::kEnd);
   if (!resident) return KVCRUSH_ERR_CUDA;
-  // what a block does once takes as long as about five tiles
-  const int n_blk = choose_cluster(resident, attend_units(a, kRows), (a.s.max_seqlen + (a.K_new.ptr ? a.fresh.most : 0) + kKeys - 1) / kKeys, 5);
+  // what a block does once takes as long as about ten tiles
+  const int n_blk = choose_cluster(resident, attend_units(a, kRows), (a.s.max_seqlen + (a.K_new.ptr ? a.fresh.most : 0) + kKeys - 1) / kKeys, 10);
   dim3 grid;
   if (!attend_grid(a, kRows, n_blk, &grid)) return KVCRUSH_ERR_UNSUPPORTED;
   return launch_chained(kern, grid, dim3(kThreads), M::kEnd, stream, n_blk, maps[0], maps[1], maps[2], maps[3], a);
@@ -501,7 +548,7 @@ int launch_one(const AttendArgs& a, const CUtensorMap (&maps)[4], cudaStream_t s
 
 bool attend_tree_fits(const AttendArgs& a) {
   const long long rows = (long long)a.fresh.most * a.s.G;
-  return a.pages.page_size == 0 && (a.K.dtype == KVCRUSH_BF16 || a.K.dtype == KVCRUSH_FP16) && a.s.D <= 128 && rows > 32 &&
+  return a.pages.page_size == 0 && (a.K.dtype == KVCRUSH_BF16 || a.K.dtype == KVCRUSH_FP16) && a.s.D <= 128 && rows > 16 &&
          a.s.max_seqlen >= 2 * kKeys && a.scale_log2 > 0.f;
 }
 
