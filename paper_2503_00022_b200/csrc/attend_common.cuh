@@ -30,6 +30,10 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 struct Unit {
   int layer, seq, hk;
   int first;                 // packed index of the first new token of the unit
@@ -143,9 +147,11 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
   const int n_pages = (w.seen + p.page_size - 1) / p.page_size;
   const int want = min(p.budget, n_pages);
   if (n_pages > want) {
+    if (n_blk > 1) cluster_arrive_relaxed();           // waited for before the first store to a peer: all blocks run then
     const unsigned char* q = static_cast<const unsigned char*>(a.Q.ptr) + bytes_of<FQ>(w.layer * a.Q.sl + w.first * a.Q.st + (long long)w.hk * s.G * a.Q.sh);
     for (int c = tid; c < s.D; c += kThreads) {
       double up = 0., down = 0.;
+#pragma unroll 8
       for (int h = 0; h < s.G; ++h) {
         const double x = widen1<FQ>(q, h * a.Q.sh + c);
         up += x > 0. || !(x == x) ? x : 0.;
@@ -154,6 +160,7 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
       mem.up[c] = up; mem.down[c] = down;
     }
     __syncthreads();
+    if (n_blk > 1) cluster_wait();
     // scores of this block's pages; eight lanes a page
     const int per = (n_pages + n_blk - 1) / n_blk, p_lo = min(n_pages, rank * per), p_hi = min(n_pages, p_lo + per);
     const int sub = lane & 7;
@@ -181,18 +188,12 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
       }
 #pragma unroll
       for (int d = 1; d < 8; d <<= 1) score += __shfl_xor_sync(kAll, score, d);
-      if (sub == 0 && page < p_hi)
-        mem.keys[page] = page < p.keep_initial || page >= n_pages - p.keep_recent ? kDecreed : score_key(score);
+      // to every block: the page's eight lanes share the work
+      const unsigned long long key = page < p.keep_initial || page >= n_pages - p.keep_recent ? kDecreed : score_key(score);
+      if (page < p_hi)
+        for (int b = sub; b < n_blk; b += 8) *(n_blk > 1 ? cluster.map_shared_rank(mem.keys + page, b) : mem.keys + page) = key;
     }
-    // every block takes the other blocks' keys
-    if (n_blk > 1) {
-      cluster.sync();
-      for (int i = tid; i < n_pages; i += kThreads) {
-        const int owner = i / per;
-        if (owner != rank) mem.keys[i] = *cluster.map_shared_rank(mem.keys + i, owner);
-      }
-    }
-    __syncthreads();
+    if (n_blk > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
     // The want-th largest key.  Scores differ little in their leading bits, so the search starts at the highest bit in which
     // any two keys differ (those read by decree apart) and goes on eight bits at a time until the keys that share the
     // bits found so far are all taken.
@@ -305,10 +306,6 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
 // A part of a row: maximum and sum of the weights, what its output is relative to, and the sum of weights times zeros.
 struct Part { float m, l, m2, b; };
 
-__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 // Where a block receives the parts of its share of the output: four channels of a row make an element.
 template <int kRows, int kMaxD>
 struct Received {
@@ -402,10 +399,10 @@ constexpr int kMaxDevices = 64;
 // device grants).
 struct ClusterTable {
   std::atomic<int> held[kMaxDevices][kMaxCluster + 1];
-  // The current device's row, after the kernel may be launched with up to `bound` bytes of dynamic shared memory; NULL where
-  // something failed.
+  // The current device's row, for launches with `dyn` bytes of dynamic shared memory, after the kernel may be launched with up to
+  // `bound`; NULL where something failed.
   template <class Kernel>
-  const std::atomic<int>* resident(Kernel kern, int threads, int bound) {
+  const std::atomic<int>* resident(Kernel kern, int threads, int dyn, int bound) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return nullptr; }
     std::atomic<int>* row = held[dev];
@@ -416,7 +413,7 @@ struct ClusterTable {
       cudaLaunchConfig_t cfg{};
       cfg.gridDim = dim3(c);
       cfg.blockDim = dim3(threads);
-      cfg.dynamicSmemBytes = bound;
+      cfg.dynamicSmemBytes = dyn;
       cudaLaunchAttribute at[1];
       at[0].id = cudaLaunchAttributeClusterDimension;
       at[0].val.clusterDim.x = c; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;

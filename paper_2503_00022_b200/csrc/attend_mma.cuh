@@ -866,8 +866,10 @@ int launch_one(AttendArgs& a, cudaStream_t stream) {
   constexpr int most = (M::kEnd + 15) / 16 * 16;
   const size_t dyn = most + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
   constexpr int bound = most + (kPages ? kMaxPagesPerSeq * 12 + 256 * 16 + 2048 : 0);
-  static ClusterTable table;
-  const std::atomic<int>* resident = table.resident(kern, kWarps * 32, bound);
+  // one table for launches that leave room for two blocks an SM, one for those with many pages
+  static ClusterTable table, large;
+  constexpr int two = bound < 113 * 1024 ? bound : 113 * 1024;
+  const std::atomic<int>* resident = dyn <= (size_t)two ? table.resident(kern, kWarps * 32, two, bound) : large.resident(kern, kWarps * 32, bound, bound);
   if (!resident) return KVCRUSH_ERR_CUDA;
   // what a block does once takes as long as about three tiles of each of its warps
   const int n_blk = choose_cluster(resident, attend_units(a, M::kRows), attend_tiles(a), 3 * kWarps);

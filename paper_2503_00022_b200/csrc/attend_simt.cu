@@ -252,7 +252,8 @@ int launch_one(AttendArgs& a, cudaStream_t stream) {
   const Shape& s = a.s;
   const size_t dyn = kOBytes + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
   static ClusterTable table;
-  const std::atomic<int>* resident = table.resident(kern, kWarps * 32, kOBytes + (kPages ? (int)page_mem_bytes(kMaxPagesPerSeq, kMaxPagesPerSeq, kMaxD) : 0));
+  const int bound = kOBytes + (kPages ? (int)page_mem_bytes(kMaxPagesPerSeq, kMaxPagesPerSeq, kMaxD) : 0);
+  const std::atomic<int>* resident = table.resident(kern, kWarps * 32, bound, bound);
   if (!resident) return KVCRUSH_ERR_CUDA;
   const int n_blk = choose_cluster(resident, attend_units(a, kRows), attend_tiles(a), 2 * kWarps);
   dim3 grid;

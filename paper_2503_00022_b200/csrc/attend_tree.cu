@@ -535,7 +535,7 @@ int launch_one(const AttendArgs& a, const CUtensorMap (&maps)[4], cudaStream_t s
   using M = TreeMem<DP>;
   auto kern = attend_tree_kernel<FQ, DP>;
   static ClusterTable table;
-  const std::atomic<int>* resident = table.resident(kern, kThreads, M::kEnd);
+  const std::atomic<int>* resident = table.resident(kern, kThreads, M::kEnd, M::kEnd);
   if (!resident) return KVCRUSH_ERR_CUDA;
   // what a block does once takes as long as about ten tiles
   const int n_blk = choose_cluster(resident, attend_units(a, kRows), (a.s.max_seqlen + (a.K_new.ptr ? a.fresh.most : 0) + kKeys - 1) / kKeys, 10);
