@@ -484,7 +484,8 @@ int kvcrush_page_bounds(const kvcrush_problem_t* problem, const kvcrush_tensor_t
  * K_new); a token that sees L rows chooses among its ceil(L / page_size) pages:
  *   score(p) = sum over channels c of hi[p][c] * a[c] + lo[p][c] * b[c],
  *   a[c], b[c] = the sums, over the query heads of the KV head's group, of the positive and of the negative q[h][c]
- * (the heads' upper bounds on q . k, added up; float64; terms with a = 0 or b = 0 are left out, a NaN counts as +inf).
+ * (the heads' upper bounds on q . k, added up, to 2^-44 of the sum of the terms' magnitudes; terms with a = 0 or b = 0
+ * are left out, a NaN counts as +inf).
  * The first keep_initial and the last keep_recent pages come before all others (lower page first), then pages by
  * score (ties: lower page); the first `budget` of this order are attended to, or all of them if there are fewer.
  *   lo, hi         as kvcrush_page_bounds writes them, of Q's type; total rows n_seqs * max_pages

@@ -119,17 +119,21 @@ struct PageMem {
   int* chosen;                               // [min(budget, max_pages)]
   double* up;                                // [D]: sum of the positive query values of the group's heads
   double* down;                              // [D]
+  float4* split;                             // the same sums as pairs of floats (up, its rest, down, its rest), see split_at
   int* count;                                // [256 + 64] counters
 };
+// The lanes that share a page read these sums 8 channels apart; 16 bytes between them keep them in different banks.
+__host__ __device__ inline int split_at(int c) { return c + (c >> 3); }
 __host__ __device__ inline size_t page_mem_bytes(int max_pages, int budget, int D) {
-  return (size_t)max_pages * 8 + (size_t)D * 16 + (((size_t)(budget < max_pages ? budget : max_pages) + 3) / 4 * 4 + 320) * 4;
+  return ((size_t)max_pages + 1) / 2 * 16 + (size_t)D * 16 + (size_t)split_at(D) * 16 + (((size_t)(budget < max_pages ? budget : max_pages) + 3) / 4 * 4 + 320) * 4;
 }
 __device__ __forceinline__ PageMem page_mem(unsigned char* base, int max_pages, int budget, int D) {
   PageMem m;
   m.keys = reinterpret_cast<unsigned long long*>(base);
-  m.up = reinterpret_cast<double*>(m.keys + max_pages);
+  m.up = reinterpret_cast<double*>(m.keys + (max_pages + 1) / 2 * 2);
   m.down = m.up + D;
-  m.count = reinterpret_cast<int*>(m.down + D);
+  m.split = reinterpret_cast<float4*>(m.down + D);
+  m.count = reinterpret_cast<int*>(m.split + split_at(D));
   m.chosen = m.count + 320;
   return m;
 }
@@ -158,40 +162,82 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
         down += x < 0. ? x : 0.;
       }
       mem.up[c] = up; mem.down[c] = down;
+      const float u = (float)up, d = (float)down;
+      mem.split[split_at(c)] = make_float4(u, (float)(up - (double)u), d, (float)(down - (double)d));
     }
     __syncthreads();
     if (n_blk > 1) cluster_wait();
     // scores of this block's pages; eight lanes a page
     const int per = (n_pages + n_blk - 1) / n_blk, p_lo = min(n_pages, rank * per), p_hi = min(n_pages, p_lo + per);
+    // Sums of pairs of floats, 2^-45 of the terms' size (the chip has next to no float64): a product and what it was rounded by,
+    // a sum and what it was rounded by.  The bounds of two pages and up to 128 channels are loaded before the first is used.
     const int sub = lane & 7;
-    for (int base = p_lo + warp * 4; base < p_hi; base += kWarps * 4) {
-      const int page = base + (lane >> 3);
-      double score = 0.;
-      if (page < p_hi) {
-        const long long row = (long long)w.seq * p.max_pages + page;
-        const unsigned char* lp = static_cast<const unsigned char*>(p.lo.ptr) + bytes_of<FQ>(w.layer * p.lo.sl + row * p.lo.st + w.hk * p.lo.sh);
-        const unsigned char* hp = static_cast<const unsigned char*>(p.hi.ptr) + bytes_of<FQ>(w.layer * p.hi.sl + row * p.hi.st + w.hk * p.hi.sh);
-        for (int c = sub * 8; c < s.D; c += 64) {
-          Raw8<FQ> lo, hi;
-          lo.load(lp + bytes_of<FQ>(c));
-          hi.load(hp + bytes_of<FQ>(c));
-          float x[8], y[8];
-          lo.widen(x);
-          hi.widen(y);
+    constexpr int kPages2 = 2, kBlocks64 = 2;
+    for (int base = p_lo + warp * 4; base < p_hi; base += kPages2 * kWarps * 4) {
+      float sum[kPages2], rest[kPages2];
+      const unsigned char *lp[kPages2], *hp[kPages2];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const double up = mem.up[c + i], down = mem.down[c + i];
-            if (up != 0.) score = fma((double)y[i], up, score);
-            if (down != 0.) score = fma((double)x[i], down, score);
+      for (int g = 0; g < kPages2; ++g) {
+        sum[g] = rest[g] = 0.f;
+        const long long row = (long long)w.seq * p.max_pages + min(base + g * kWarps * 4 + (lane >> 3), p_hi - 1);
+        lp[g] = static_cast<const unsigned char*>(p.lo.ptr) + bytes_of<FQ>(w.layer * p.lo.sl + row * p.lo.st + w.hk * p.lo.sh);
+        hp[g] = static_cast<const unsigned char*>(p.hi.ptr) + bytes_of<FQ>(w.layer * p.hi.sl + row * p.hi.st + w.hk * p.hi.sh);
+      }
+      for (int c0 = 0; c0 < s.D; c0 += 64 * kBlocks64) {
+        Raw8<FQ> lo[kPages2][kBlocks64], hi[kPages2][kBlocks64];
+#pragma unroll
+        for (int g = 0; g < kPages2; ++g)
+#pragma unroll
+          for (int b = 0; b < kBlocks64; ++b) {
+            const int c = min(c0 + b * 64 + sub * 8, s.D - 8);       // channels that there are; those beyond count as zeros below
+            lo[g][b].load(lp[g] + bytes_of<FQ>(c));
+            hi[g][b].load(hp[g] + bytes_of<FQ>(c));
+          }
+#pragma unroll
+        for (int b = 0; b < kBlocks64; ++b) {
+          const int c = c0 + b * 64 + sub * 8;
+          if (c < s.D) {
+            float x[kPages2][8], y[kPages2][8];
+#pragma unroll
+            for (int g = 0; g < kPages2; ++g) { lo[g][b].widen(x[g]); hi[g][b].widen(y[g]); }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float4 q = mem.split[split_at(c + i)];
+#pragma unroll
+              for (int g = 0; g < kPages2; ++g)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const float a = k ? q.z : q.x, a_rest = k ? q.w : q.y, v = a == 0.f ? 0.f : k ? x[g][i] : y[g][i];
+                  const float t = a * v, t_rest = fmaf(a, v, -t), next = sum[g] + t, back = next - sum[g];
+                  rest[g] += ((sum[g] - (next - back)) + (t - back)) + fmaf(a_rest, v, t_rest);
+                  sum[g] = next;
+                }
+            }
           }
         }
       }
 #pragma unroll
-      for (int d = 1; d < 8; d <<= 1) score += __shfl_xor_sync(kAll, score, d);
-      // to every block: the page's eight lanes share the work
-      const unsigned long long key = page < p.keep_initial || page >= n_pages - p.keep_recent ? kDecreed : score_key(score);
-      if (page < p_hi)
-        for (int b = sub; b < n_blk; b += 8) *(n_blk > 1 ? cluster.map_shared_rank(mem.keys + page, b) : mem.keys + page) = key;
+      for (int g = 0; g < kPages2; ++g) {
+        const int page = base + g * kWarps * 4 + (lane >> 3);
+        double score = (double)sum[g] + (double)rest[g];
+        // out of float32's range, or near its end: the definition itself
+        if (!(fabsf(sum[g]) < 0x1p100f) || fabsf(sum[g]) < 0x1p-60f) {
+          score = 0.;
+#pragma unroll 1
+          for (int c0 = sub * 8; c0 < s.D; c0 += 64)
+#pragma unroll 1
+            for (int c = c0; c < c0 + 8; ++c) {
+              if (mem.up[c] != 0.) score = fma(widen1<FQ>(hp[g], c), mem.up[c], score);
+              if (mem.down[c] != 0.) score = fma(widen1<FQ>(lp[g], c), mem.down[c], score);
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) score += __shfl_xor_sync(kAll, score, d);
+        // to every block: the page's eight lanes share the work
+        const unsigned long long key = page < p.keep_initial || page >= n_pages - p.keep_recent ? kDecreed : score_key(score);
+        if (page < p_hi)
+          for (int b = sub; b < n_blk; b += 8) *(n_blk > 1 ? cluster.map_shared_rank(mem.keys + page, b) : mem.keys + page) = key;
+      }
     }
     if (n_blk > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
     // The want-th largest key.  Scores differ little in their leading bits, so the search starts at the highest bit in which
@@ -364,10 +410,11 @@ __device__ __forceinline__ void join_and_write(const AttendArgs& a, const Unit& 
   for (int i = tid; i < min(per, total - mine); i += kThreads) {
     const int e = mine + i, row = e / vec, d = (e - row * vec) * 4;
     float M = neg_inf();
+#pragma unroll 8
     for (int p = 0; p < n_blk; ++p) M = fmaxf(M, recv->part[p * kRows + row].m);
     float l = 0.f, b = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
     for (int p = 0; p < n_blk; ++p) {
       const Part q = recv->part[p * kRows + row];
       const float4 v = recv->o[p * per + i];

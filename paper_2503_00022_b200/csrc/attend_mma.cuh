@@ -653,9 +653,6 @@ attend_kernel(AttendArgs a) {
     }
     copies_commit();
   };
-#pragma unroll
-  for (int i = 0; i < M::kStages - 1; ++i) fetch(lo + warp + i * kWarps, i);
-
   // queries: DP / 8 lanes take a row, a lane eight channels; all rows are loaded before the first is used
   {
     constexpr int kLanes = DP / 8, kPerStep = kWarps * 32 / kLanes, kQSteps = (kRows + kPerStep - 1) / kPerStep;
@@ -669,6 +666,9 @@ attend_kernel(AttendArgs a) {
       if (r < w.rows && d < s.D)
         raw[u].load(static_cast<const unsigned char*>(a.Q.ptr) + bytes_of<FQ>(w.layer * a.Q.sl + (w.first + w.token(r)) * a.Q.st + (w.hk * s.G + w.head(r)) * a.Q.sh + d));
     }
+    // the first tiles are under way while the queries arrive
+#pragma unroll
+    for (int i = 0; i < M::kStages - 1; ++i) fetch(lo + warp + i * kWarps, i);
 #pragma unroll
     for (int u = 0; u < kQSteps; ++u) {
       const int r = r0 + u * kPerStep;
