@@ -98,42 +98,56 @@ __device__ __forceinline__ bool sees_new(const AttendArgs& a, const Unit& w, int
 
 // ---- the choice of pages ----------------------------------------------------------------------------------
 
-// Larger score, larger key; every score below the pages that are read by decree.
+// Scores are sums of pairs of floats, good to 2^-45 of their terms' size: this chip has next to no float64 arithmetic (one
+// instruction of a warp in 32 clocks of an SM).
+struct Pair { float sum, rest; };
+// a + x, and what the sum was rounded by
+__device__ __forceinline__ void add_to(Pair& a, float x, float x_rest) {
+  const float next = a.sum + x, back = next - a.sum;
+  a.rest += ((a.sum - (next - back)) + (x - back)) + x_rest;
+  a.sum = next;
+}
+// Larger score, larger key, every score below the pages that are read by decree: the bits of the score as a float64.
+__device__ __forceinline__ unsigned long long bits_key(unsigned long long b) { return b & 0x8000000000000000ull ? ~b : b | 0x8000000000000000ull; }
 __device__ __forceinline__ unsigned long long score_key(double x) {
   if (!(x == x)) return 0xFFF0000000000000ull;                      // counts as +inf
-  const unsigned long long b = (unsigned long long)__double_as_longlong(x + 0.0);
-  return b & 0x8000000000000000ull ? ~b : b | 0x8000000000000000ull;
+  return bits_key((unsigned long long)__double_as_longlong(x + 0.0));
+}
+// The same of a pair, 2^-60 <= |sum| < 2^100, by integers: the sum's bits, and the rest in units of the float64's last place.
+__device__ __forceinline__ unsigned long long score_key(const Pair& p) {
+  const float s = p.sum + p.rest, r = p.rest - (s - p.sum);
+  const uint32_t b = __float_as_uint(s);
+  const int e = (int)(b >> 23 & 255u) - 127;
+  const int k = __float2int_rn(r * __uint_as_float((uint32_t)(52 - e + 127) << 23));
+  const unsigned long long magnitude = ((unsigned long long)(b & 0x7FFFFFFFu) << 29) + (896ull << 52) + (unsigned long long)(long long)(b >> 31 ? -k : k);
+  return bits_key(magnitude | (unsigned long long)(b >> 31) << 63);
 }
 constexpr unsigned long long kDecreed = ~0ull;
 
 template <int FQ>
-__device__ __forceinline__ double widen1(const void* p, long long i) {
-  if constexpr (FQ == KVCRUSH_FP32) return (double)static_cast<const float*>(p)[i];
-  else if constexpr (FQ == KVCRUSH_BF16) return (double)__bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-  else return (double)__half2float(static_cast<const __half*>(p)[i]);
+__device__ __forceinline__ float widen1(const void* p, long long i) {
+  if constexpr (FQ == KVCRUSH_FP32) return static_cast<const float*>(p)[i];
+  else if constexpr (FQ == KVCRUSH_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+  else return __half2float(static_cast<const __half*>(p)[i]);
 }
 
 // Shared memory of the choice: keys of all pages, the chosen pages, and coefficients of the channels.
 struct PageMem {
   unsigned long long* keys;                  // [max_pages]
   int* chosen;                               // [min(budget, max_pages)]
-  double* up;                                // [D]: sum of the positive query values of the group's heads
-  double* down;                              // [D]
-  float4* split;                             // the same sums as pairs of floats (up, its rest, down, its rest), see split_at
+  float4* sums;                              // sums of the group's positive and of its negative query values (pairs), see sums_at
   int* count;                                // [256 + 64] counters
 };
 // The lanes that share a page read these sums 8 channels apart; 16 bytes between them keep them in different banks.
-__host__ __device__ inline int split_at(int c) { return c + (c >> 3); }
+__host__ __device__ inline int sums_at(int c) { return c + (c >> 3); }
 __host__ __device__ inline size_t page_mem_bytes(int max_pages, int budget, int D) {
-  return ((size_t)max_pages + 1) / 2 * 16 + (size_t)D * 16 + (size_t)split_at(D) * 16 + (((size_t)(budget < max_pages ? budget : max_pages) + 3) / 4 * 4 + 320) * 4;
+  return ((size_t)max_pages + 1) / 2 * 16 + (size_t)sums_at(D) * 16 + (((size_t)(budget < max_pages ? budget : max_pages) + 3) / 4 * 4 + 320) * 4;
 }
 __device__ __forceinline__ PageMem page_mem(unsigned char* base, int max_pages, int budget, int D) {
   PageMem m;
   m.keys = reinterpret_cast<unsigned long long*>(base);
-  m.up = reinterpret_cast<double*>(m.keys + (max_pages + 1) / 2 * 2);
-  m.down = m.up + D;
-  m.split = reinterpret_cast<float4*>(m.down + D);
-  m.count = reinterpret_cast<int*>(m.split + split_at(D));
+  m.sums = reinterpret_cast<float4*>(m.keys + (max_pages + 1) / 2 * 2);
+  m.count = reinterpret_cast<int*>(m.sums + sums_at(D));
   m.chosen = m.count + 320;
   return m;
 }
@@ -154,31 +168,28 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
     if (n_blk > 1) cluster_arrive_relaxed();           // waited for before the first store to a peer: all blocks run then
     const unsigned char* q = static_cast<const unsigned char*>(a.Q.ptr) + bytes_of<FQ>(w.layer * a.Q.sl + w.first * a.Q.st + (long long)w.hk * s.G * a.Q.sh);
     for (int c = tid; c < s.D; c += kThreads) {
-      double up = 0., down = 0.;
+      Pair up{0.f, 0.f}, down{0.f, 0.f};
 #pragma unroll 8
       for (int h = 0; h < s.G; ++h) {
-        const double x = widen1<FQ>(q, h * a.Q.sh + c);
-        up += x > 0. || !(x == x) ? x : 0.;
-        down += x < 0. ? x : 0.;
+        const float x = widen1<FQ>(q, h * a.Q.sh + c);
+        add_to(up, x > 0.f || !(x == x) ? x : 0.f, 0.f);
+        add_to(down, x < 0.f ? x : 0.f, 0.f);
       }
-      mem.up[c] = up; mem.down[c] = down;
-      const float u = (float)up, d = (float)down;
-      mem.split[split_at(c)] = make_float4(u, (float)(up - (double)u), d, (float)(down - (double)d));
+      mem.sums[sums_at(c)] = make_float4(up.sum, up.rest, down.sum, down.rest);
     }
     __syncthreads();
     if (n_blk > 1) cluster_wait();
     // scores of this block's pages; eight lanes a page
     const int per = (n_pages + n_blk - 1) / n_blk, p_lo = min(n_pages, rank * per), p_hi = min(n_pages, p_lo + per);
-    // Sums of pairs of floats, 2^-45 of the terms' size (the chip has next to no float64): a product and what it was rounded by,
-    // a sum and what it was rounded by.  The bounds of two pages and up to 128 channels are loaded before the first is used.
+    // The bounds of two pages and up to 128 channels are loaded before the first is used.
     const int sub = lane & 7;
     constexpr int kPages2 = 2, kBlocks64 = 2;
     for (int base = p_lo + warp * 4; base < p_hi; base += kPages2 * kWarps * 4) {
-      float sum[kPages2], rest[kPages2];
+      Pair score[kPages2];
       const unsigned char *lp[kPages2], *hp[kPages2];
 #pragma unroll
       for (int g = 0; g < kPages2; ++g) {
-        sum[g] = rest[g] = 0.f;
+        score[g] = Pair{0.f, 0.f};
         const long long row = (long long)w.seq * p.max_pages + min(base + g * kWarps * 4 + (lane >> 3), p_hi - 1);
         lp[g] = static_cast<const unsigned char*>(p.lo.ptr) + bytes_of<FQ>(w.layer * p.lo.sl + row * p.lo.st + w.hk * p.lo.sh);
         hp[g] = static_cast<const unsigned char*>(p.hi.ptr) + bytes_of<FQ>(w.layer * p.hi.sl + row * p.hi.st + w.hk * p.hi.sh);
@@ -202,15 +213,14 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
             for (int g = 0; g < kPages2; ++g) { lo[g][b].widen(x[g]); hi[g][b].widen(y[g]); }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              const float4 q = mem.split[split_at(c + i)];
+              const float4 q = mem.sums[sums_at(c + i)];
 #pragma unroll
               for (int g = 0; g < kPages2; ++g)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                   const float a = k ? q.z : q.x, a_rest = k ? q.w : q.y, v = a == 0.f ? 0.f : k ? x[g][i] : y[g][i];
-                  const float t = a * v, t_rest = fmaf(a, v, -t), next = sum[g] + t, back = next - sum[g];
-                  rest[g] += ((sum[g] - (next - back)) + (t - back)) + fmaf(a_rest, v, t_rest);
-                  sum[g] = next;
+                  const float t = a * v;
+                  add_to(score[g], t, fmaf(a_rest, v, fmaf(a, v, -t)));
                 }
             }
           }
@@ -219,22 +229,29 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
 #pragma unroll
       for (int g = 0; g < kPages2; ++g) {
         const int page = base + g * kWarps * 4 + (lane >> 3);
-        double score = (double)sum[g] + (double)rest[g];
-        // out of float32's range, or near its end: the definition itself
-        if (!(fabsf(sum[g]) < 0x1p100f) || fabsf(sum[g]) < 0x1p-60f) {
-          score = 0.;
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) {
+          const float o = __shfl_xor_sync(kAll, score[g].sum, d), o_rest = __shfl_xor_sync(kAll, score[g].rest, d);
+          add_to(score[g], o, o_rest);
+        }
+        unsigned long long key = page < p.keep_initial || page >= n_pages - p.keep_recent ? kDecreed : score_key(score[g]);
+        // a score that is out of float32's range, or near its end: by float64
+        const bool out = key != kDecreed && (!(fabsf(score[g].sum) < 0x1p100f) || fabsf(score[g].sum) < 0x1p-60f);
+        if (__any_sync(kAll, out)) {
+          double exact = 0.;
 #pragma unroll 1
-          for (int c0 = sub * 8; c0 < s.D; c0 += 64)
+          for (int c0 = sub * 8; out && c0 < s.D; c0 += 64)
 #pragma unroll 1
             for (int c = c0; c < c0 + 8; ++c) {
-              if (mem.up[c] != 0.) score = fma(widen1<FQ>(hp[g], c), mem.up[c], score);
-              if (mem.down[c] != 0.) score = fma(widen1<FQ>(lp[g], c), mem.down[c], score);
+              const float4 q = mem.sums[sums_at(c)];
+              if (q.x != 0.f) exact = fma((double)widen1<FQ>(hp[g], c), (double)q.x + (double)q.y, exact);
+              if (q.z != 0.f) exact = fma((double)widen1<FQ>(lp[g], c), (double)q.z + (double)q.w, exact);
             }
-        }
 #pragma unroll
-        for (int d = 1; d < 8; d <<= 1) score += __shfl_xor_sync(kAll, score, d);
+          for (int d = 1; d < 8; d <<= 1) exact += __shfl_xor_sync(kAll, exact, d);
+          if (out) key = score_key(exact);
+        }
         // to every block: the page's eight lanes share the work
-        const unsigned long long key = page < p.keep_initial || page >= n_pages - p.keep_recent ? kDecreed : score_key(score);
         if (page < p_hi)
           for (int b = sub; b < n_blk; b += 8) *(n_blk > 1 ? cluster.map_shared_rank(mem.keys + page, b) : mem.keys + page) = key;
       }

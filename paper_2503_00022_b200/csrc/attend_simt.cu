@@ -176,7 +176,7 @@ attend_simt_kernel(AttendArgs a) {
   if (n_blk > 1) cluster_arrive_relaxed();
   for (int e = tid; e < kRows * s.D; e += kWarps * 32) {
     const int r = e / s.D, d = e - r * s.D;
-    q_sh[r * kMaxD + d] = r < w.rows ? (float)widen1<FQ>(a.Q.ptr, w.layer * a.Q.sl + (w.first + w.token(r)) * a.Q.st +
+    q_sh[r * kMaxD + d] = r < w.rows ? widen1<FQ>(a.Q.ptr, w.layer * a.Q.sl + (w.first + w.token(r)) * a.Q.st +
                                                                      (w.hk * s.G + w.head(r)) * a.Q.sh + d) : 0.f;
   }
   __syncthreads();
