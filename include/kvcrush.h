@@ -450,7 +450,7 @@ typedef struct kvcrush_new_tokens {
  *                  FP32; K_new and V_new both or none
  *   K, V           the cache: of Q's type (scales NULL) or quantised, both in the same type
  *   lse_out_dev    optional out [n_layers][n_q_heads][total_new] float32, natural log
- * head_dim <= 256, a multiple of 8 (quantised caches: see kvcrush_quantize); less than 2^31 bytes from a token to the next.
+ * O must not overlap an input.  head_dim <= 256, a multiple of 8 (quantised caches: see kvcrush_quantize); less than 2^31 bytes from a token to the next.
  * Without new tokens (total_new 0) nothing is
  * done; K and V of a problem without rows may have NULL pointers.  A token that sees no row, or whose logits are
  * all -inf, gets zeros and a log-sum-exp of -inf.  Rows that a token does not see have no influence on its output,

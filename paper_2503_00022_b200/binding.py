@@ -434,14 +434,23 @@ class CompressionPass:
     page_size > 0 selects and gathers whole pages of that many tokens: budgets then count pages,
     ``idx`` holds page numbers, the reduced cache has page_size rows per kept page and keep_initial /
     keep_recent count pages as well.
+
+    cache_format INT8, E4M3 or INT4 (kept tokens, not pages) quantises the reduced cache as it is written: ``k_out`` and
+    ``v_out`` are then QuantTensors.  spare_rows leaves room behind each sequence's kept rows, so that new tokens can be
+    appended (``kvcrush_quantize`` with out_begin = ``row_begin + row_count``); kvcrush_attend reads the cache with
+    ``row_begin`` and ``row_count`` [layers, sequences].
     """
 
     def __init__(self, problem: Problem, budget_imp: np.ndarray, budget_rep: np.ndarray,
                  cache_dtype=None, sig_keep: Optional[np.ndarray] = None, anchor_mode=ANCHOR_ALTERNATE,
                  anchor_bits: Optional[np.ndarray] = None, impl=SCORE_AUTO, with_kind=True, with_cache=True,
                  pool_kernel: int = 0, keep_recent: int = 0, page_size: int = 0, keep_initial: int = 0,
-                 share_importance: bool = True):
+                 share_importance: bool = True, cache_format: Optional[int] = None, spare_rows: int = 0):
         import torch
+        if cache_format is not None and page_size:
+            raise ValueError("a quantised reduced cache holds kept tokens, not pages")
+        if spare_rows and cache_format is None:
+            raise ValueError("only a quantised reduced cache is written with room behind its sequences")
         self.page_size = int(page_size)
         unit = max(self.page_size, 1)
         p = self.problem = problem
@@ -483,7 +492,17 @@ class CompressionPass:
         nbytes = max(kvcrush_workspace_size(p, st) for st in (STAGE_SCORE, STAGE_SIGNATURE, STAGE_SELECT))
         self.workspace = torch.empty((max(nbytes, 256),), dtype=torch.uint8, device=dev)
         self.k_out = self.v_out = None
-        if with_cache and cache_dtype is not None:
+        self.cache_format = cache_format
+        # where the kept rows of a sequence start in their layer, and how many there are
+        rows = kept * unit
+        begin = np.zeros((Lyr, S), dtype=np.int64)
+        begin[:, 1:] = np.cumsum(rows + spare_rows, axis=1)[:, :-1]
+        self.row_begin = torch.from_numpy(begin.astype(np.int32)).to(dev)
+        self.row_count = torch.from_numpy(rows.astype(np.int32)).to(dev)
+        if with_cache and cache_format is not None:
+            n_out = max(int((rows + spare_rows).sum(axis=1).max()), 1)
+            self.k_out, self.v_out = (QuantTensor.empty(Lyr, n_out, p.n_kv_heads, p.head_dim, cache_format, device=dev) for _ in range(2))
+        elif with_cache and cache_dtype is not None:
             n_out = int(self.kept_per_layer.max()) * unit if Lyr else 0
             shape = (Lyr, max(n_out, 1), p.n_kv_heads, p.head_dim)
             self.k_out = torch.empty(shape, dtype=cache_dtype, device=dev)
@@ -526,6 +545,10 @@ class CompressionPass:
                        workspace=self.workspace, status=self.status)
 
     def compact(self, k_cache, v_cache):
+        if self.cache_format is not None:
+            kvcrush_quantize(self.problem, k_cache, v_cache, self.k_out, self.v_out, cu_kept=self.cu_kept, idx=self.idx,
+                             total_kept=self.total_kept, out_begin=self.row_begin, status=self.status)
+            return
         if self.page_size:
             kvcrush_compact_pages(self.problem, k_cache, v_cache, self.page_size, self.cu_kept, self.idx,
                                   self.total_kept, self.k_out, self.v_out, status=self.status)

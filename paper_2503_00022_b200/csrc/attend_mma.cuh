@@ -858,14 +858,18 @@ attend_kernel(AttendArgs a) {
 
 template <int F, int FQ, int DP, int NB, bool kPages>
 int launch_one(AttendArgs& a, cudaStream_t stream) {
-  // Two blocks an SM: a chip has room for 14 clusters of 16 then, with one only for 7.
-  constexpr int kWarps = NB * DP <= 128 && (kQuantized<F> || DP == 64) ? 8 : 4, kBlocks = Mem<F, FQ, DP, NB, kWarps, kPages>::kEnd <= 113 * 1024 ? 2 : 1;
+  // Eight warps where the registers of two blocks an SM hold them (a chip has room for 14 clusters of 16 then, with one
+  // block only for 7); two where 256 channels of 16 bits have to leave room for the choice of pages.
+  constexpr bool kWide = DP == 256 && !kQuantized<F>;
+  constexpr int kWarps = NB * DP <= 128 && (kQuantized<F> || DP == 64) ? 8 : kPages && kWide ? 2 : 4;
+  constexpr int kBlocks = Mem<F, FQ, DP, NB, kWarps, kPages>::kEnd <= 113 * 1024 ? 2 : 1;
   auto kern = attend_kernel<F, FQ, DP, NB, kWarps, kBlocks, kPages>;
   using M = Mem<F, FQ, DP, NB, kWarps, kPages>;
   const Shape& s = a.s;
   constexpr int most = (M::kEnd + 15) / 16 * 16;
   const size_t dyn = most + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
   constexpr int bound = most + (kPages ? kMaxPagesPerSeq * 12 + 256 * 16 + 2048 : 0);
+  static_assert(bound <= 227 * 1024, "shared memory of a block");
   // one table for launches that leave room for two blocks an SM, one for those with many pages
   static ClusterTable table, large;
   constexpr int two = bound < 113 * 1024 ? bound : 113 * 1024;

@@ -233,6 +233,10 @@ PAGED = [
     ("fp32", None, 64, 4, 2, (260, 17), (1, 2), 8, 4, 0, 1),
     ("fp32", C.INT8, 32, 2, 1, (100,), (1,), 8, 1, 0, 0),
     ("bf16", None, 40, 40, 1, (200,), (2,), 64, 2, 0, 0),
+    ("fp16", None, 256, 20, 1, (210, 9), (1, 1), 8, 9, 1, 1),
+    ("bf16", None, 192, 2, 2, (300,), (1,), 16, 4, 0, 2),
+    ("bf16", C.INT4, 256, 4, 1, (260,), (2,), 16, 5, 0, 1),
+    ("fp32", C.E4M3, 256, 2, 1, (90,), (1,), 8, 3, 0, 0),
 ]
 
 
@@ -420,3 +424,87 @@ def test_negative_scale(B):
             n = 500 - 9 + 1 + i
             o, lse, _, _ = C.attend_row(c.q64[0, i, x], c.k64[0, :n, x // 8], c.v64[0, :n, x // 8], -0.1)
             assert np.abs(out[0, i, x] - o).max() < 0.01 and abs(float(c.lse[0, x, i]) - lse) < 1e-3
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 2), ("fp16", 30), ("fp32", 3)])
+def test_heads_that_share_memory(B, dtype, n):
+    """A stride of 0 along the heads of the cache and of the new tokens (the TMA unit cannot take it)."""
+    c = Case(B, dtype, None, 64, 8, 4, (300,), (n,), own=True, seed=28)
+    c.k, c.v, c.kn, c.vn = (x[:, :, :1].expand(-1, -1, 4, -1) for x in (c.k, c.v, c.kn, c.vn))
+    c.k64, c.v64 = TL.numpy64(c.k), TL.numpy64(c.v)
+    c.run(B.NewTokens((n,)))
+    c.check(lambda l, s, i, h: (np.arange(300), np.arange(i + 1)))
+
+
+@pytest.mark.parametrize("pages,page", [(8192, 8), (3000, 16)])
+@pytest.mark.parametrize("dtype,fmt,D,Hq,Hkv", [("bf16", None, 64, 2, 1), ("fp16", C.INT4, 32, 1, 1), ("fp32", None, 8, 2, 1), ("bf16", None, 136, 1, 1)])
+def test_many_pages(B, dtype, fmt, D, Hq, Hkv, pages, page):
+    """As many pages as a sequence may have, budgets from one page to nearly all of them."""
+    import torch
+    L = pages * page - 3
+    c = Case(B, dtype, fmt, D, Hq, Hkv, (L,), (1,), seed=29)
+    lo, hi = (torch.zeros((1, pages, Hkv, D), dtype=c.q.dtype, device="cuda:0") for _ in range(2))
+    B.kvcrush_page_bounds(c.prob, c.k_dense, page, lo, hi, status=c.status)
+    lo64, hi64 = TL.numpy64(lo), TL.numpy64(hi)
+    for budget in (1, 100, pages - 1):
+        idx = torch.zeros((1, 1, Hkv, budget), dtype=torch.int32, device="cuda:0")
+        B.kvcrush_attend_pages(c.prob, B.NewTokens((1,)), c.q, c.k, c.v, page, lo, hi, budget, c.out, keep_recent=1, page_idx=idx,
+                               lse=c.lse, status=c.status)
+
+        def visible(l, s, i, h):
+            q = c.q64[0, 0]
+            up, down = np.where(q > 0, q, 0).sum(0), np.where(q < 0, q, 0).sum(0)
+            scores = hi64[0, :, h] @ up + lo64[0, :, h] @ down
+            chosen = C.choose_pages(scores, budget, 0, 1)
+            assert idx.cpu().numpy().reshape(-1).tolist() == chosen.tolist()
+            rows = (chosen[:, None] * page + np.arange(page)).reshape(-1)
+            return rows[rows < L], []
+
+        c.check(visible)
+
+
+def test_scores_at_the_ends_of_the_range(B):
+    """Scores beyond float32 and far below 1 are ordered as float64 orders them."""
+    import torch
+    for qs, ks in ((2.0 ** 100, 2.0 ** 60), (2.0 ** -60, 2.0 ** -50), (2.0 ** -100, 2.0 ** 60)):
+        c = Case(B, "bf16", None, 64, 4, 2, (400,), (1,), seed=30, gain=ks)
+        c.q *= qs
+        c.q64 = TL.numpy64(c.q)
+        lo, hi = (torch.zeros((1, 50, 2, 64), dtype=c.q.dtype, device="cuda:0") for _ in range(2))
+        B.kvcrush_page_bounds(c.prob, c.k, 8, lo, hi, status=c.status)
+        idx = torch.zeros((1, 1, 2, 7), dtype=torch.int32, device="cuda:0")
+        B.kvcrush_attend_pages(c.prob, B.NewTokens((1,)), c.q, c.k, c.v, 8, lo, hi, 7, c.out, page_idx=idx, status=c.status)
+        for h in range(2):
+            scores = C.page_scores(c.q64[0, 0, 2 * h:2 * h + 2], TL.numpy64(lo)[0, :, h], TL.numpy64(hi)[0, :, h])
+            assert idx[0, 0, h].cpu().numpy().tolist() == C.choose_pages(scores, 7, 0, 0).tolist()
+
+
+@pytest.mark.parametrize("dtype,fmt,n", [("bf16", None, 1), ("fp16", None, 40), ("bf16", C.INT8, 2), ("fp16", C.INT4, 1), ("fp32", None, 1)])
+def test_rows_beyond_four_gigabytes(B, dtype, fmt, n):
+    """A token stride of a mebibyte: the last rows of the cache lie more than 2^32 bytes from its start."""
+    import torch
+    L, D, page = 4400, 64, 8
+    c = Case(B, dtype, fmt, D, 2, 1, (L,), (n,), own=True, seed=33)
+
+    def spread(t):
+        step = (1 << 20) // t.element_size()
+        big = torch.zeros(L * step, dtype=t.dtype, device="cuda:0")
+        view = big.as_strided((1, L, 1, t.shape[3]), (L * step, step, t.shape[3], 1))
+        view.copy_(t)
+        return view
+
+    if fmt is None:
+        c.k, c.v = spread(c.k), spread(c.v)
+    else:
+        c.k, c.v = (B.QuantTensor(spread(x.codes), x.scales, fmt) for x in (c.k, c.v))
+    c.run(B.NewTokens((n,)))
+    c.check(lambda l, s, i, h: (np.arange(L), np.arange(i + 1)))
+    if fmt is None:
+        lo, hi = (torch.zeros((1, L // page, 1, D), dtype=c.q.dtype, device="cuda:0") for _ in range(2))
+        B.kvcrush_page_bounds(c.prob, c.k, page, lo, hi, status=c.status)
+        a, b = C.page_bounds(c.k64[0, :, 0], page)
+        assert np.array_equal(TL.numpy64(lo)[0, :, 0], a) and np.array_equal(TL.numpy64(hi)[0, :, 0], b)
+    else:
+        back = torch.zeros((1, L, 1, D), dtype=torch.float32, device="cuda:0")
+        B.kvcrush_dequantize(c.prob, c.k, None, back, None, status=c.status)
+        assert np.allclose(TL.numpy64(back), c.k64, rtol=2.0 ** -22, atol=2.0 ** -21)
