@@ -11,6 +11,7 @@ using namespace kvc;
 constexpr int kMaxHeadDim = 256;
 constexpr int kMaxNew = 1024;
 constexpr int kMaxPageSize = 1024;
+constexpr uint32_t kWaitPolls = 1u << 20, kShortWaitPolls = 1u << 12;   // limits of a barrier wait
 constexpr long long kMaxStep = 1LL << 31;            // bytes from one token to the next, in the attention kernels
 
 // Values (scales NULL) or codes with their scales.  `empty`: no row of it is read, so that it may have no memory.
@@ -115,6 +116,7 @@ int make_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* ne
   a->row_count = row_count_dev;
   a->lse = lse_out_dev;
   a->status = status_dev;
+  a->polls = kWaitPolls;
   const float scale = problem->softmax_scale != 0.f ? problem->softmax_scale : 1.f / sqrtf((float)s.D);
   a->scale_log2 = scale * 1.4426950408889634f;
   return KVCRUSH_OK;
@@ -162,12 +164,16 @@ int kvcrush_dequantize(const kvcrush_problem_t* problem, const kvcrush_tensor_t*
                        out_begin_dev, status_dev, stream);
 }
 
-int kvcrush_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* new_tokens, const kvcrush_tensor_t* Q,
-                   const kvcrush_tensor_t* K, const kvcrush_scales_t* K_scales,
-                   const kvcrush_tensor_t* V, const kvcrush_scales_t* V_scales,
-                   const kvcrush_tensor_t* K_new, const kvcrush_tensor_t* V_new,
-                   const int32_t* row_begin_dev, const int32_t* row_count_dev,
-                   const kvcrush_tensor_t* O, float* lse_out_dev, int32_t* status_dev, void* stream) {
+}  // extern "C"
+
+namespace {
+
+int attend_entry(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* new_tokens, const kvcrush_tensor_t* Q,
+                 const kvcrush_tensor_t* K, const kvcrush_scales_t* K_scales,
+                 const kvcrush_tensor_t* V, const kvcrush_scales_t* V_scales,
+                 const kvcrush_tensor_t* K_new, const kvcrush_tensor_t* V_new,
+                 const int32_t* row_begin_dev, const int32_t* row_count_dev,
+                 const kvcrush_tensor_t* O, float* lse_out_dev, int32_t* status_dev, void* stream, bool short_waits, bool withhold) {
   AttendArgs a{};
   int rc = make_attend(problem, new_tokens, Q, K, K_scales, V, V_scales, row_begin_dev, row_count_dev, O, lse_out_dev, status_dev, &a);
   if (rc != KVCRUSH_OK || a.fresh.total == 0) return rc;
@@ -178,7 +184,34 @@ int kvcrush_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t*
     if (a.K_new.st * elt_bytes(a.Q.dtype) >= kMaxStep || a.V_new.st * elt_bytes(a.Q.dtype) >= kMaxStep) return KVCRUSH_ERR_UNSUPPORTED;
     if (a.K_new.dtype != a.Q.dtype || a.V_new.dtype != a.Q.dtype) return KVCRUSH_ERR_INVALID_ARG;
   }
+  if (short_waits) a.polls = kShortWaitPolls;
+  a.withhold = withhold;
   return dispatch_attend(a, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvcrush_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* new_tokens, const kvcrush_tensor_t* Q,
+                   const kvcrush_tensor_t* K, const kvcrush_scales_t* K_scales,
+                   const kvcrush_tensor_t* V, const kvcrush_scales_t* V_scales,
+                   const kvcrush_tensor_t* K_new, const kvcrush_tensor_t* V_new,
+                   const int32_t* row_begin_dev, const int32_t* row_count_dev,
+                   const kvcrush_tensor_t* O, float* lse_out_dev, int32_t* status_dev, void* stream) {
+  return attend_entry(problem, new_tokens, Q, K, K_scales, V, V_scales, K_new, V_new, row_begin_dev, row_count_dev, O, lse_out_dev,
+                      status_dev, stream, false, false);
+}
+
+// Not part of the public ABI (the header does not declare it): kvcrush_attend for the test that makes a bounded wait run out.
+// short_waits: the barrier waits of the kernel for many query rows give up after a few thousand polls; withhold: its producer
+// stops before its first copy, so that the other roles' first waits run out with nothing in flight and every block returns with
+// status = {KVCRUSH_DEV_TIMEOUT, kernel id, block, 0}.  Other kernels have no such waits.
+int kvcrush_diag_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* new_tokens, const kvcrush_tensor_t* Q,
+                        const kvcrush_tensor_t* K, const kvcrush_tensor_t* V, const kvcrush_tensor_t* K_new, const kvcrush_tensor_t* V_new,
+                        const kvcrush_tensor_t* O, int32_t* status_dev, void* stream, int short_waits, int withhold) {
+  return attend_entry(problem, new_tokens, Q, K, nullptr, V, nullptr, K_new, V_new, nullptr, nullptr, O, nullptr, status_dev, stream,
+                      short_waits != 0, withhold != 0);
 }
 
 int kvcrush_page_bounds(const kvcrush_problem_t* problem, const kvcrush_tensor_t* K, int page_size, int recent_pages,

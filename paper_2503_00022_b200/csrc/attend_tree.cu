@@ -29,7 +29,6 @@ constexpr int kKeys = 64;                    // keys of a tile
 constexpr int kThreads = 384;                // producer, an issuer for each stream, helper, two softmax warpgroups
 constexpr int kExtra = 8;                    // keys added at a time by the rows' threads
 constexpr float kSlackLog2 = 8.f;
-constexpr uint32_t kPolls = tc::kWaitPolls;
 
 template <int DP>
 struct TreeMem {
@@ -157,17 +156,17 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
   if (warp == 0) {
     int issued = 0;
-    if (lane == 0) {
+    if (lane == 0 && !a.withhold) {
       for (; issued < n; ++issued) {
         const int st = issued % M::kStages, round = issued / M::kStages;
         const bool is_new = lo + issued >= cached;
         const int row = is_new ? w.first + (lo + issued - cached) * kKeys : w.begin + (lo + issued) * kKeys;
         const uint32_t kb = tc::smem_u32(&aux->k_full[st]), vb = tc::smem_u32(issued < n_full ? &aux->v_full[st] : &aux->masked_full[st]);
         const uint32_t kd = base + M::kRing + st * 2 * M::kTileBytes, vd = kd + M::kTileBytes;
-        if (round > 0 && !mbar_wait(tc::smem_u32(&aux->k_empty[st]), (round - 1) & 1, abort_flag, kPolls)) break;
+        if (round > 0 && !mbar_wait(tc::smem_u32(&aux->k_empty[st]), (round - 1) & 1, abort_flag, a.polls)) break;
         tc::mbar_expect_tx(kb, M::kTileBytes);
         for (int b = 0; b < M::kBlocks; ++b) tc::tma_load_4d(kd + b * kKeys * 128, is_new ? &map_kn : &map_k, kb, b * 64, row, w.hk, w.layer);
-        if (round > 0 && !mbar_wait(tc::smem_u32(&aux->v_empty[st]), (round - 1) & 1, abort_flag, kPolls)) {
+        if (round > 0 && !mbar_wait(tc::smem_u32(&aux->v_empty[st]), (round - 1) & 1, abort_flag, a.polls)) {
           for (uint32_t i = 0; i < tc::kDrainPolls && !tc::mbar_try_wait(kb, round & 1); ++i) {}
           break;
         }
@@ -193,7 +192,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const uint64_t desc_q = tc::smem_desc_sw128(base + M::kQ), desc_k = tc::smem_desc_sw128(base + M::kRing);
       const uint64_t desc_v = values_desc(base + M::kRing + M::kTileBytes);
       auto wait = [&](unsigned long long* bar, int parity) {
-        return (bool)__all_sync(kAll, mbar_wait(tc::smem_u32(bar), parity, abort_flag, kPolls));
+        return (bool)__all_sync(kAll, mbar_wait(tc::smem_u32(bar), parity, abort_flag, a.polls));
       };
       auto product_s = [&](int t, int st, int parity) {
         const int u = t >> 1;
@@ -252,7 +251,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     // values of the masked tiles: a lane looks at rows lane and lane + 32
     for (int t = n_full; t < n; ++t) {
       const int st = t % M::kStages, keys = keys_of(t);
-      if (!__all_sync(kAll, mbar_wait(tc::smem_u32(&aux->masked_full[st]), ((t - n_full) / M::kStages) & 1, abort_flag, kPolls))) break;
+      if (!__all_sync(kAll, mbar_wait(tc::smem_u32(&aux->masked_full[st]), ((t - n_full) / M::kStages) & 1, abort_flag, a.polls))) break;
       for (int h = lane; h < kKeys; h += 32) {
         unsigned char* vd = sh + M::kRing + st * 2 * M::kTileBytes + M::kTileBytes + h * 128;    // row h of every block of channels
         bool bad = false;
@@ -305,7 +304,7 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     };
     bool ok = true;
     auto wait = [&](unsigned long long* bar, int parity) {             // one answer for the warp
-      return (bool)__all_sync(kAll, mbar_wait(tc::smem_u32(bar), parity, abort_flag, kPolls));
+      return (bool)__all_sync(kAll, mbar_wait(tc::smem_u32(bar), parity, abort_flag, a.polls));
     };
     // the output so far, times f (a factor for each row)
     auto scale_output = [&](float f) {

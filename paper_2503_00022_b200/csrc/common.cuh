@@ -258,6 +258,8 @@ struct AttendArgs {
   float* lse;
   float scale_log2;
   int32_t* status;
+  uint32_t polls;                  // limit of a barrier wait in attend_tree.cu
+  int withhold;                    // diagnostic, there: the producer stops before its first copy
   uint32_t group_magic;            // row / G = row * group_magic >> 32 (G > 1)
   PageChoice pages;                  // page_size 0: every row is read
 };

@@ -508,3 +508,25 @@ def test_rows_beyond_four_gigabytes(B, dtype, fmt, n):
         back = torch.zeros((1, L, 1, D), dtype=torch.float32, device="cuda:0")
         B.kvcrush_dequantize(c.prob, c.k, None, back, None, status=c.status)
         assert np.allclose(TL.numpy64(back), c.k64, rtol=2.0 ** -22, atol=2.0 ** -21)
+
+
+@pytest.mark.parametrize("lens", [(700,), (40, 300)])
+def test_a_bounded_wait_that_runs_out_is_reported(B, lens):
+    """The producer of the kernel for many query rows stops before its first copy: nothing is in flight, every role's first wait
+    gives up, the kernel returns and says so, and the same call succeeds once the status word is cleared."""
+    import ctypes
+    import torch
+    counts = (12,) * len(lens)
+    c = Case(B, "bf16", None, 128, 8, 2, lens, counts, own=True, seed=34)
+    new = B.NewTokens(counts)
+    fn = B.lib().kvcrush_diag_attend
+    fn.argtypes, fn.restype = [ctypes.c_void_p] * 10 + [ctypes.c_int] * 2, ctypes.c_int
+    call = lambda withhold: fn(c.prob.address, new.ref, *(B._packed(t) for t in (c.q, c.k, c.v, c.kn, c.vn, c.out)),   # noqa: E731
+                               c.status.data_ptr(), B._stream(), 1, withhold)
+    assert call(1) == 0
+    torch.cuda.synchronize()
+    st = c.status.cpu().tolist()
+    assert st[0] == B.DEV_TIMEOUT and st[1] == 5
+    c.status.zero_()
+    c.run(new)
+    c.check(lambda l, s, i, h: (np.arange(c.cu[s], c.cu[s + 1]), np.arange(i + 1)))
