@@ -547,10 +547,10 @@ struct Mem {
   static constexpr int kRecv = kPart + kWarps * kRows * (int)sizeof(Part);
   static constexpr int kRing = (kRecv + (int)sizeof(Received<kRows, DP>) + 127) / 128 * 128;
   static constexpr int kO = kRing;
-  // At most 96 KB of rings a block, less where two blocks would not fit an SM (the choice of pages needs room too): as many stages as that holds, two at least, and
+  // Rings as large as two blocks an SM allow (the choice of pages needs room too): as many stages as that holds, two at least, and
   // room for a tile of 16-bit new tokens.
   static constexpr int kStageBytes = (Stage<F, DP>::kBytes + 127) / 128 * 128;
-  static constexpr int kWarpBytes = (kPages ? 64 * 1024 : kRing > 16 * 1024 ? 112 * 1024 - kRing : 96 * 1024) / kWarps;
+  static constexpr int kWarpBytes = (kPages ? 64 * 1024 : 113 * 1024 - kRing) / kWarps;
   static constexpr int kStages = kWarpBytes / kStageBytes < 2 ? 2 : kWarpBytes / kStageBytes > 6 ? 6 : kWarpBytes / kStageBytes;
   static constexpr int kNewBytes = kQuantized<F> ? Stage<FQ, DP>::kBytes : 0;
   static constexpr int kRingBytes = kStages * kStageBytes > kNewBytes ? kStages * kStageBytes : kNewBytes;
@@ -632,7 +632,7 @@ attend_kernel(AttendArgs a) {
     }
     return h;
   };
-  // The ring: while a tile is multiplied the next kStages - 1 are under way.  Tiles of new tokens go through it too where they are of
+  // The ring: while a tile is multiplied the next kStages - 1 are under way, and its place is filled again behind it.  Tiles of new tokens go through it too where they are of
   // the cache's type.
   using T = Stage<F, DP>;
   const uint32_t ring = smem_addr(sh + M::kRing) + warp * M::kRingBytes;
@@ -668,7 +668,7 @@ attend_kernel(AttendArgs a) {
     }
     // the first tiles are under way while the queries arrive
 #pragma unroll
-    for (int i = 0; i < M::kStages - 1; ++i) fetch(lo + warp + i * kWarps, i);
+    for (int i = 0; i < M::kStages; ++i) fetch(lo + warp + i * kWarps, i);
 #pragma unroll
     for (int u = 0; u < kQSteps; ++u) {
       const int r = r0 + u * kPerStep;
@@ -757,9 +757,8 @@ attend_kernel(AttendArgs a) {
   };
   int stage = 0;
   for (int t = lo + warp; t < hi_ring; t += kWarps) {
-    copies_wait<M::kStages - 2>();
+    copies_wait<M::kStages - 1>();
     __syncwarp();
-    fetch(t + (M::kStages - 1) * kWarps, stage == 0 ? M::kStages - 1 : stage - 1);
     const uint32_t at = ring + stage * M::kStageBytes;
     float x[NB][4];
     logits<F, A, DP, NB, kRegs>(at, q, qr, lane, x);
@@ -791,8 +790,9 @@ attend_kernel(AttendArgs a) {
       }
     }
     add_tile<F, F, A, DP, NB>(at, h, s.D, x, hidden, run, lane);
-    stage = stage == M::kStages - 1 ? 0 : stage + 1;
     __syncwarp();
+    fetch(t + M::kStages * kWarps, stage);
+    stage = stage == M::kStages - 1 ? 0 : stage + 1;
   }
   if constexpr (kInteger<F>) {                         // from units of the integer products to values
 #pragma unroll
