@@ -12,13 +12,17 @@
  *                                                            (Algorithm 2, Sec. 3, Sec. 3.2)
  *   kvcrush_compact    gather of the kept K/V rows into the reduced cache (Sec. 3.2)
  *
+ * What reads the reduced cache afterwards is here too: kvcrush_quantize / kvcrush_dequantize keep it in 8 or 4 bits,
+ * kvcrush_attend is the attention of generated or drafted tokens over it, kvcrush_page_bounds and kvcrush_attend_pages
+ * read only the pages that a token asks for.
+ *
  * Conventions for every entry point unless stated otherwise
  *   - Pointers named *_dev (and every tensor / output pointer) are DEVICE pointers
  *     owned by the caller; pointers named *_host are host pointers read during the
  *     call only.  The library allocates and frees no memory and keeps no state
- *     between calls apart from four process-wide, write-once caches (the driver's
+ *     between calls apart from five process-wide, write-once caches (the driver's
  *     tensor-map encoder entry point; how many thread block clusters of the window
- *     kernel a device holds at once, and whether it runs those of the selection; for
+ *     kernel and of the attention kernels a device holds at once, and whether it runs those of the selection; for
  *     kvcrush_signature_static the device address of its array); scratch memory is the caller's `workspace` (device, 256-byte
  *     aligned, size from kvcrush_workspace_size).
  *   - Work is enqueued on `stream` (a cudaStream_t passed as void*, NULL = default

@@ -2,6 +2,8 @@
 //
 // A warp takes tiles of 16 keys against up to eight query rows: the four lanes of a quad share a key's row for the
 // logits, the 32 lanes share the channels for the output, and the weights pass between the two through shared memory.
+// Float32 queries only, over caches of any type.  Seven drafted tokens of 8 heads of 64 over 1001 float32 rows: 13 us; bound by the
+// chain of a tile (one warp a scheduler, every key of a tile in turn for the output).
 #include "attend_common.cuh"
 
 namespace kvc {
