@@ -49,7 +49,7 @@ def decode(codes: np.ndarray, scales: np.ndarray, fmt: int) -> np.ndarray:
         return codes.view(np.int8).astype(np.float64) * s[..., None]
     if fmt == E4M3:
         return e4m3_value(codes) * s[..., None]
-    n = np.stack([codes & 15, codes >> 4], axis=-1).reshape(codes.shape[:-1] + (-1,)).astype(np.float64)
+    n = np.stack([codes & 15, codes >> 4], axis=-1).reshape(codes.shape[:-1] + (2 * codes.shape[-1],)).astype(np.float64)
     return n * s[..., :1] + s[..., 1:]
 
 

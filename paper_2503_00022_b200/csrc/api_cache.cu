@@ -14,19 +14,30 @@ constexpr int kMaxPageSize = 1024;
 constexpr uint32_t kWaitPolls = 1u << 20, kShortWaitPolls = 1u << 12;   // limits of a barrier wait
 constexpr long long kMaxStep = 1LL << 31;            // bytes from one token to the next, in the attention kernels
 
+// A tensor that nothing is read from or written to may have no memory.
+alignas(16) const unsigned char kNowhere[16] = {};
+int make_view(const kvcrush_tensor_t* t, int head_dim, bool empty, TensorView* v) {
+  kvcrush_tensor_t some;
+  if (empty && t && !t->ptr_dev) {
+    some = *t;
+    some.ptr_dev = const_cast<unsigned char*>(kNowhere);
+    t = &some;
+  }
+  return view_from_tensor(t, head_dim, v);
+}
+
 // Values (scales NULL) or codes with their scales.  `empty`: no row of it is read, so that it may have no memory.
 int make_cache(const kvcrush_tensor_t* t, const kvcrush_scales_t* scales, int head_dim, bool empty, CacheView* c) {
   kvcrush_tensor_t some;
   kvcrush_scales_t some_scales;
-  alignas(16) static const unsigned char nowhere[16] = {};
   if (empty && t && !t->ptr_dev) {
     some = *t;
-    some.ptr_dev = nowhere;
+    some.ptr_dev = const_cast<unsigned char*>(kNowhere);
     t = &some;
   }
   if (empty && scales && !scales->ptr_dev) {
     some_scales = *scales;
-    some_scales.ptr_dev = reinterpret_cast<float*>(const_cast<unsigned char*>(nowhere));
+    some_scales.ptr_dev = reinterpret_cast<float*>(const_cast<unsigned char*>(kNowhere));
     scales = &some_scales;
   }
   if (!scales) {
@@ -65,15 +76,16 @@ int convert_entry(const kvcrush_problem_t* problem, bool quantize, const kvcrush
   if ((V_val == nullptr) != (V_codes == nullptr) || (V_val == nullptr) != (V_scales == nullptr)) return KVCRUSH_ERR_INVALID_ARG;
   if (cu_kept_dev ? total_kept < 0 : idx_dev != nullptr) return KVCRUSH_ERR_INVALID_ARG;
   if (s.D > kMaxHeadDim || s.D % 8) return KVCRUSH_ERR_UNSUPPORTED;
+  const RowList rows{cu_kept_dev, idx_dev, cu_kept_dev ? (long long)total_kept : (long long)s.n_layers * s.T, in_begin_dev, out_begin_dev};
+  const bool none = rows.total == 0;
   CacheView kv{}, vv{}, kc{}, vc{};
-  if ((rc = make_cache(K_val, nullptr, s.D, false, &kv)) != KVCRUSH_OK) return rc;
-  if ((rc = make_cache(K_codes, K_scales, s.D, false, &kc)) != KVCRUSH_OK) return rc;
+  if ((rc = make_cache(K_val, nullptr, s.D, none, &kv)) != KVCRUSH_OK) return rc;
+  if ((rc = make_cache(K_codes, K_scales, s.D, none, &kc)) != KVCRUSH_OK) return rc;
   if (V_val) {
-    if ((rc = make_cache(V_val, nullptr, s.D, false, &vv)) != KVCRUSH_OK) return rc;
-    if ((rc = make_cache(V_codes, V_scales, s.D, false, &vc)) != KVCRUSH_OK) return rc;
+    if ((rc = make_cache(V_val, nullptr, s.D, none, &vv)) != KVCRUSH_OK) return rc;
+    if ((rc = make_cache(V_codes, V_scales, s.D, none, &vc)) != KVCRUSH_OK) return rc;
     if (vv.dtype != kv.dtype || vc.dtype != kc.dtype) return KVCRUSH_ERR_INVALID_ARG;
   }
-  const RowList rows{cu_kept_dev, idx_dev, cu_kept_dev ? (long long)total_kept : (long long)s.n_layers * s.T, in_begin_dev, out_begin_dev};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return quantize ? launch_convert_rows(s, kv, vv, rows, kc, vc, st) : launch_convert_rows(s, kc, vc, rows, kv, vv, st);
 }
@@ -223,11 +235,12 @@ int kvcrush_page_bounds(const kvcrush_problem_t* problem, const kvcrush_tensor_t
   if (!status_dev || page_size < 1 || recent_pages < 0 || (row_begin_dev == nullptr) != (row_count_dev == nullptr))
     return KVCRUSH_ERR_INVALID_ARG;
   TensorView k, l, h;
-  if ((rc = view_from_tensor(K, s.D, &k)) != KVCRUSH_OK) return rc;
-  if ((rc = view_from_tensor(lo, s.D, &l)) != KVCRUSH_OK) return rc;
-  if ((rc = view_from_tensor(hi, s.D, &h)) != KVCRUSH_OK) return rc;
+  if ((rc = make_view(K, s.D, s.T == 0, &k)) != KVCRUSH_OK) return rc;
+  if ((rc = make_view(lo, s.D, s.T == 0, &l)) != KVCRUSH_OK) return rc;
+  if ((rc = make_view(hi, s.D, s.T == 0, &h)) != KVCRUSH_OK) return rc;
   if (l.dtype != k.dtype || h.dtype != k.dtype) return KVCRUSH_ERR_INVALID_ARG;
   if (page_size % 8 || page_size > kMaxPageSize || s.D > kMaxHeadDim || s.D % 8) return KVCRUSH_ERR_UNSUPPORTED;
+  if (s.T == 0) return KVCRUSH_OK;
   return launch_page_bounds(s, k, page_size, recent_pages, row_begin_dev, row_count_dev, l, h, static_cast<cudaStream_t>(stream));
 }
 
@@ -243,8 +256,8 @@ int kvcrush_attend_pages(const kvcrush_problem_t* problem, const kvcrush_new_tok
   if (rc != KVCRUSH_OK || a.fresh.total == 0) return rc;
   if (a.fresh.mask || page_size < 1 || budget < 1 || keep_initial < 0 || keep_recent < 0) return KVCRUSH_ERR_INVALID_ARG;
   PageChoice& p = a.pages;
-  if ((rc = view_from_tensor(lo, a.s.D, &p.lo)) != KVCRUSH_OK) return rc;
-  if ((rc = view_from_tensor(hi, a.s.D, &p.hi)) != KVCRUSH_OK) return rc;
+  if ((rc = make_view(lo, a.s.D, a.s.T == 0, &p.lo)) != KVCRUSH_OK) return rc;
+  if ((rc = make_view(hi, a.s.D, a.s.T == 0, &p.hi)) != KVCRUSH_OK) return rc;
   if (p.lo.dtype != a.Q.dtype || p.hi.dtype != a.Q.dtype) return KVCRUSH_ERR_INVALID_ARG;
   if (page_size % 8 || page_size > kMaxPageSize || pages_of(a.s, page_size) > kMaxPagesPerSeq) return KVCRUSH_ERR_UNSUPPORTED;
   p.page_size = page_size; p.budget = budget; p.keep_initial = keep_initial; p.keep_recent = keep_recent;

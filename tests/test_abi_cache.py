@@ -145,3 +145,37 @@ def test_pages_refuse_bad_arguments(lib):
     assert pages(n=_new(mask=0x100, words=1)) == INV and pages(q=f) == INV
     assert pages(page=8, prob=_problem(cu=(0, 70000))) == UNS                     # more than 8192 pages
     assert pages(n=_new(cu=(0, 0)), q=_t(ptr=None)) == 0
+
+
+def test_pages_of_an_empty_cache_need_no_memory(lib):
+    """A cache without rows, whose tensors have no memory: no bounds to write, and the checks of the arguments stay."""
+    none, t, p = _t(ptr=None), _t(), _problem(cu=(0, 0))
+
+    def bounds(prob=p, k=none, lo=none, hi=none, page=32, status=0x100):
+        return lib.kvcrush_page_bounds(r(prob), r(k), page, 0, None, None, r(lo), r(hi), status, None)
+
+    assert bounds() == 0
+    assert bounds(page=0) == INV and bounds(page=12) == UNS and bounds(status=None) == INV
+    assert bounds(lo=_t(B.FP16, ptr=None)) == INV and bounds(k=_t(B.INT8, ptr=None)) == INV
+    assert bounds(prob=_problem(cu=(0, 50))) == INV and bounds(prob=_problem(cu=(0, 50)), k=t) == INV
+
+    def pages(prob, lo, hi):
+        return lib.kvcrush_attend_pages(r(prob), r(_new()), r(t), r(none), None, r(none), None, 32, r(lo), r(hi), 4, 0, 0, None, None, None,
+                                        None, r(t), None, None, None)
+
+    assert pages(p, none, none) == INV                                            # no status word
+
+
+def test_rows_of_an_empty_list_need_no_memory(lib):
+    """Quantising no rows, from and into tensors without memory, is a call like any other; the types are checked all the same."""
+    t, c, s = _t(ptr=None), _t(B.INT8, ptr=None), _s(ptr=None)
+
+    def both(want, prob=_problem(cu=(0, 0)), val=t, cu=None, total=0):
+        assert lib.kvcrush_quantize(r(prob), r(val), r(val), cu, None, total, None, None, r(c), r(s), r(c), r(s), 0x100, None) == want
+        assert lib.kvcrush_dequantize(r(prob), r(c), r(s), r(c), r(s), cu, None, total, None, None, r(val), r(val), 0x100, None) == want
+
+    both(0)
+    both(0, prob=_problem(), cu=0x100)
+    both(INV, prob=_problem())
+    both(INV, prob=_problem(), cu=0x100, total=1)
+    both(INV, val=c)

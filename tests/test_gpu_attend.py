@@ -530,3 +530,18 @@ def test_a_bounded_wait_that_runs_out_is_reported(B, lens):
     c.status.zero_()
     c.run(new)
     c.check(lambda l, s, i, h: (np.arange(c.cu[s], c.cu[s + 1]), np.arange(i + 1)))
+
+
+@pytest.mark.parametrize("dtype,fmt", (("bf16", None), ("fp16", C.INT4), ("fp32", None)))
+def test_pages_of_an_empty_cache(B, dtype, fmt):
+    """No row at all: no page is chosen, the output is zero, and tensors without rows need no memory."""
+    import torch
+    c = Case(B, dtype, fmt, 64, 4, 2, (0, 0), (1, 2), layers=2, seed=81)
+    lo, hi = (torch.empty((2, 0, 2, 64), dtype=c.q.dtype, device="cuda:0") for _ in range(2))
+    B.kvcrush_page_bounds(c.prob, c.k_dense, 16, lo, hi, status=c.status)
+    idx = torch.full((2, 3, 2, 4), -7, dtype=torch.int32, device="cuda:0")
+    num = torch.full((2, 3, 2), -7, dtype=torch.int32, device="cuda:0")
+    B.kvcrush_attend_pages(c.prob, B.NewTokens((1, 2)), c.q, c.k, c.v, 16, lo, hi, 4, c.out, page_idx=idx, n_pages=num, lse=c.lse,
+                           status=c.status)
+    assert (idx == -1).all() and (num == 0).all() and (c.out == 0).all() and torch.isneginf(c.lse).all()
+    assert c.status.cpu().tolist()[0] == 0
