@@ -11,10 +11,11 @@
 // logit, and the weight on the other side, so that no value is ever dequantised.  Weights that carry a scale have a
 // maximum of their own (below), since the largest weight need not belong to the largest product of weight and scale.
 // Measured, 8 KV heads of 128 with 4 query heads each: one token over 2048 bf16 rows 6.4 us, over 32768 4-bit rows 25 us
-// (37.7 MB), over 16 ragged sequences of 8-bit rows 25 us (80 MB, 3.3 TB/s); 15 tokens of 32 heads of 96 over the same sequences
+// (37.7 MB), over 16 ragged sequences of 8-bit rows 25 us (80 MB, 3.2 TB/s); 15 tokens of 32 heads of 96 over the same sequences
 // in float16 103 us (472 MB, 4.6 TB/s).  Few units are bound by what one warp does for a tile one thing after the other (about
-// 300 instructions and 1650 clocks for 4-bit codes, 208 instructions for 16-bit values, at 7 to 8 warps an SM) and by what a block
-// does once: 1000 clocks to find its unit, 2500 for queries and first tiles, 3500 to 5000 for the join.
+// 300 instructions and 1400 to 1700 clocks for 4-bit codes, 208 instructions for 16-bit values, at 7 to 8 warps an SM) and by what a block
+// does once: 750 to 1000 clocks to find its unit, 1000 to 5000 for queries and first tiles, 2800 to 10000 for the join, which
+// waits for the slowest block.
 #pragma once
 
 #include "attend_common.cuh"

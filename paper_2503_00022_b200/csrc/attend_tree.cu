@@ -14,9 +14,9 @@
 // a tile first: rows that do not exist or hold a value that is not finite are cleared, and in the second case the whole tile
 // gets weight 0 and the threads of the rows add its keys one by one at the end.
 // Trees over 32768 rows of 8 KV heads of 128, 4 query heads each (135 MB, 20.6 us at the measured copy bandwidth): 9 to 16 tokens
-// 40 us, 63 tokens (34 GFLOP) 61 us, where attend_mma.cuh takes 82 to 89 and 151; 2048 rows, 63 tokens 15 against 20; 16 ragged
-// sequences of 1192 to 4085 rows, 16 tokens 53 against 80.  In the 61 us tensor and special-function pipes are busy for 40 % on
-// 96 SMs: two tiles of rows x 8 heads make 16 units, of which the chip holds clusters of six blocks and no larger ones.
+// 40 to 41 us, 63 tokens (34 GFLOP) 62 us, where attend_mma.cuh takes 82 to 89 and 151; 2048 rows, 63 tokens 15 against 20; 16 ragged
+// sequences of 1192 to 4085 rows, 16 tokens 53 against 80.  In the 62 us tensor and special-function pipes are busy for 40 % on
+// 96 SMs: two tiles of rows x 8 heads make 16 units, of which the chip holds clusters of six blocks (22, but 15 of seven).
 #include "attend_common.cuh"
 #include "tc_ptx.cuh"
 
@@ -43,7 +43,7 @@ struct TreeMem {
   static constexpr int kRecvO = kRing;                                  // outputs of the peers, when the ring is done with
   static constexpr int kRecvPart = kRing + 2 * kStages * kTileBytes + 256;
   static constexpr int kAux = kRecvPart + kMaxCluster * kRows * 8;
-  static constexpr int kEnd = kAux + 3072;
+  static constexpr int kEnd = kAux + 3 * 1024;
   static_assert(kRows * DP * 4 + kMaxCluster * 16 <= 2 * kStages * kTileBytes + 256, "room for the peers' outputs");
   static_assert(kEnd <= 227 * 1024, "one block an SM");
 };
@@ -54,7 +54,7 @@ struct TreeAux {
   uint32_t tmem;
   int abort_flag, slow;                      // slow: bit i, masked tile i of this block is added key by key
 };
-static_assert(sizeof(TreeAux) <= 3072, "auxiliary memory");
+static_assert(sizeof(TreeAux) <= 3 * 1024, "auxiliary memory");
 
 // Descriptor of 16 keys x 64 or 128 channels of values: rows of 64 channels (128 bytes, 128-byte swizzle), eight keys 1024 bytes
 // apart, blocks of 64 channels kKeys rows apart.

@@ -5,9 +5,9 @@
 // head) belongs to 4, 8 or 16 lanes with one to three pieces of eight channels each; its largest magnitude (INT4: least and
 // largest value) is found by shuffles while the row stays in registers.
 //
-// 32 layers x 2048 rows x 32 heads of 128, both tensors: bf16 to 8 bits 279 us = 5.8 TB/s
-// (591 with a row to 16 lanes, one row a warp and unpaired arithmetic), to 4 bits 301; back 263 = 6.2 TB/s and 235.  What keeps
-// the way in below the way out is arithmetic: 11 instructions a value, the ALU pipe busy for 54 %.
+// 32 layers x 2048 rows x 32 heads of 128, both tensors: bf16 to 8 bits 278 us = 5.8 TB/s
+// (591 with a row to 16 lanes, one row a warp and unpaired arithmetic), to 4 bits 298; back 261 = 6.2 TB/s and 235.  What keeps
+// the way in below the way out is arithmetic: about 12.6 instructions a value, the ALU pipe busy for 54 %.
 //
 // Codes are quotients rounded to the nearest code.  Rows of 16-bit values have few significant bits, so that quotients often
 // lie on the border between two codes exactly, and a product with a rounded reciprocal would fall on either side.  The
