@@ -412,6 +412,7 @@ typedef struct kvcrush_scales {
  *   K, V           inputs and outputs as for kvcrush_compact; V (with its scales and output) may be NULL.  Type of the
  *                  16- or 32-bit side: BF16, FP16 or FP32.  head_dim <= 256, a multiple of 8; INT8 and E4M3: of 16,
  *                  INT4: of 32
+ * Tensors and scales may have NULL pointers where there is no row (total_kept 0, or no list and no token).
  * Rows that the lists do not name are left as they were.  Two rows written to one place are a race.
  */
 int kvcrush_quantize(const kvcrush_problem_t* problem, const kvcrush_tensor_t* K, const kvcrush_tensor_t* V,
@@ -454,9 +455,8 @@ typedef struct kvcrush_new_tokens {
  *                  FP32; K_new and V_new both or none
  *   K, V           the cache: of Q's type (scales NULL) or quantised, both in the same type
  *   lse_out_dev    optional out [n_layers][n_q_heads][total_new] float32, natural log
- * O must not overlap an input.  head_dim <= 256, a multiple of 8 (quantised caches: see kvcrush_quantize); less than 2^31 bytes from a token to the next.
- * Without new tokens (total_new 0) nothing is
- * done; K and V of a problem without rows may have NULL pointers.  A token that sees no row, or whose logits are
+ * O must not overlap an input.  head_dim <= 256, a multiple of 8 (quantised caches: see kvcrush_quantize); less than 2^31
+ * bytes from a token to the next.  Without new tokens (total_new 0) nothing is done; K and V of a problem without rows may have NULL pointers.  A token that sees no row, or whose logits are
  * all -inf, gets zeros and a log-sum-exp of -inf.  Rows that a token does not see have no influence on its output,
  * whatever they hold.  Logits, softmax statistics and sums are float32; the weights are rounded to the 16-bit type that
  * they are multiplied in (FP32: not at all).  Results do not depend on what else runs, nor on the order of the blocks.
@@ -477,6 +477,7 @@ int kvcrush_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t*
  *   page_size    a multiple of 8, up to 1024
  *   recent_pages 0: all pages; n > 0: only the last n of every sequence (what a cache needs when it has grown)
  *   row_begin_dev, row_count_dev   as for kvcrush_attend
+ * K, lo and hi of a problem without rows (total_tokens 0) may have NULL pointers.
  */
 int kvcrush_page_bounds(const kvcrush_problem_t* problem, const kvcrush_tensor_t* K, int page_size, int recent_pages,
                         const int32_t* row_begin_dev, const int32_t* row_count_dev,
@@ -496,7 +497,8 @@ int kvcrush_page_bounds(const kvcrush_problem_t* problem, const kvcrush_tensor_t
  *   budget         >= 1
  *   page_idx_dev   optional out [n_layers][total_new][n_kv_heads][budget] int32: the pages, ascending, then -1
  *   n_pages_dev    optional out [n_layers][total_new][n_kv_heads] int32: how many there are
- * At most 8192 pages a sequence.  Other arguments as for kvcrush_attend (mask_dev must be NULL).
+ * At most 8192 pages a sequence.  Other arguments as for kvcrush_attend (mask_dev must be NULL); of a problem
+ * without rows, lo and hi may have NULL pointers too.
  */
 int kvcrush_attend_pages(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* new_tokens, const kvcrush_tensor_t* Q,
                          const kvcrush_tensor_t* K, const kvcrush_scales_t* K_scales,

@@ -545,3 +545,39 @@ def test_pages_of_an_empty_cache(B, dtype, fmt):
                            status=c.status)
     assert (idx == -1).all() and (num == 0).all() and (c.out == 0).all() and torch.isneginf(c.lse).all()
     assert c.status.cpu().tolist()[0] == 0
+
+
+@pytest.mark.parametrize("dtype,fmt,n,page", (("bf16", C.INT8, 1, 0), ("bf16", None, 40, 0), ("fp32", None, 3, 0), ("fp16", C.INT4, 1, 16)))
+def test_calls_at_once_on_two_streams(B, dtype, fmt, n, page):
+    """Two calls over different caches, in turn on two streams that are not the current one, give the bits of calls alone."""
+    import torch
+    cases = [Case(B, dtype, fmt, 64, 8, 2, (900, 300), (n, 1), own=not page, seed=101 + i) for i in (0, 10)]
+    new = B.NewTokens((n, 1))
+    bounds = []
+    for c in cases:
+        lo, hi = (torch.zeros((1, 2 * 57, 2, 64), dtype=c.q.dtype, device="cuda:0") for _ in range(2))
+        if page:
+            B.kvcrush_page_bounds(c.prob, c.k_dense, page, lo, hi, status=c.status)
+        bounds.append((lo, hi))
+
+    def call(i, **more):
+        c = cases[i]
+        if page:
+            B.kvcrush_attend_pages(c.prob, new, c.q, c.k, c.v, page, *bounds[i], 7, c.out, lse=c.lse, status=c.status, **more)
+        else:
+            c.run(new, **more)
+
+    alone = []
+    for i, c in enumerate(cases):
+        call(i)
+        alone.append((c.out.clone(), c.lse.clone()))
+        c.out.fill_(7.0)
+        c.lse.fill_(7.0)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            call(i, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for c, (out, lse) in zip(cases, alone):
+        assert torch.equal(c.out, out) and torch.equal(c.lse, lse) and c.status.cpu().tolist()[0] == 0
