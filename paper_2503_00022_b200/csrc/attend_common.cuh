@@ -252,7 +252,9 @@ __device__ __forceinline__ int choose_pages(const AttendArgs& a, const Unit& w, 
           for (int d = 1; d < 8; d <<= 1) exact += __shfl_xor_sync(kAll, exact, d);
           if (out) key = score_key(exact);
         }
-        // to every block: the page's eight lanes share the work
+        // To every block: the page's eight lanes share the work.  Which half of a sum a lane adds to which decides the last bits of
+        // the rest, so the lanes' keys differ there; all blocks get that of the page's first lane.
+        key = __shfl_sync(kAll, key, lane & ~7);
         if (page < p_hi)
           for (int b = sub; b < n_blk; b += 8) *(n_blk > 1 ? cluster.map_shared_rank(mem.keys + page, b) : mem.keys + page) = key;
       }
