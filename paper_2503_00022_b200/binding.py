@@ -433,7 +433,8 @@ class CompressionPass:
 
     page_size > 0 selects and gathers whole pages of that many tokens: budgets then count pages,
     ``idx`` holds page numbers, the reduced cache has page_size rows per kept page and keep_initial /
-    keep_recent count pages as well.
+    keep_recent count pages as well.  ``row_count`` leaves out the slots of a short last page that hold no token; it is
+    current from ``select`` on.
 
     cache_format INT8, E4M3 or INT4 (kept tokens, not pages) quantises the reduced cache as it is written: ``k_out`` and
     ``v_out`` are then QuantTensors.  spare_rows leaves room behind each sequence's kept rows, so that new tokens can be
@@ -498,7 +499,20 @@ class CompressionPass:
         begin = np.zeros((Lyr, S), dtype=np.int64)
         begin[:, 1:] = np.cumsum(rows + spare_rows, axis=1)[:, :-1]
         self.row_begin = torch.from_numpy(begin.astype(np.int32)).to(dev)
+        # Slots of a short last page hold no token.  Whether that page is kept only the selection knows, unless none or all are:
+        # then it is the last of the segment's list, which ascends.
+        short = lens * unit - np.asarray(p.seqlens, dtype=np.int64)[None, :]
+        rows -= np.where(kept == lens, short, 0)
+        open_ = (short > 0) & (kept > 0) & (kept < lens)
         self.row_count = torch.from_numpy(rows.astype(np.int32)).to(dev)
+        self._short_page = None
+        if open_.any():
+            end = np.where(open_, cu_kept[1:].reshape(Lyr, S) - 1, 0)      # place in the list
+            last = np.where(open_, lens - 1, -1)                           # page that is short (no page: nothing to find out)
+            full, fewer = rows, rows - np.where(open_, short, 0)
+            end, last, full, fewer = (torch.from_numpy(x.reshape(-1).astype(t)).to(dev) for x, t in (
+                (end, np.int64), (last, np.int32), (full, np.int32), (fewer, np.int32)))
+            self._short_page = (end, last, full, fewer, torch.empty_like(last), torch.empty_like(last, dtype=torch.bool))
         if with_cache and cache_format is not None:
             n_out = max(int((rows + spare_rows).sum(axis=1).max()), 1)
             self.k_out, self.v_out = (QuantTensor.empty(Lyr, n_out, p.n_kv_heads, p.head_dim, cache_format, device=dev) for _ in range(2))
@@ -537,12 +551,24 @@ class CompressionPass:
                                  n_kept=self.n_kept, anchor_mode=self.anchor_mode, anchor_bits=self.anchor_bits,
                                  keep_initial=self.keep_initial, keep_recent=self.keep_recent,
                                  workspace=self.workspace, status=self.status)
+            self._count_rows()
             return
         kvcrush_select(self.problem, sc, self.sigs, self.budget_imp,
                        self.budget_rep, self.cu_kept, self.idx, importance=imp, kind=self.kind, n_kept=self.n_kept,
                        anchor_mode=self.anchor_mode,
                        anchor_bits=self.anchor_bits, keep_recent=self.keep_recent, keep_initial=self.keep_initial,
                        workspace=self.workspace, status=self.status)
+
+    def _count_rows(self):
+        """row_count of the pages in ``idx``, where budgets and lengths alone do not tell: three small operations on the current
+        stream, into tensors that exist already."""
+        import torch
+        if self._short_page is None:
+            return
+        end, last, full, fewer, page, hit = self._short_page
+        torch.index_select(self.idx, 0, end, out=page)
+        torch.eq(page, last, out=hit)
+        torch.where(hit, fewer, full, out=self.row_count.view(-1))
 
     def compact(self, k_cache, v_cache):
         if self.cache_format is not None:
