@@ -452,6 +452,14 @@ class CompressionPass:
             raise ValueError("a quantised reduced cache holds kept tokens, not pages")
         if spare_rows and cache_format is None:
             raise ValueError("only a quantised reduced cache is written with room behind its sequences")
+        if spare_rows < 0:
+            raise ValueError("spare_rows is a number of rows")
+        if cache_format is not None:
+            unit = {INT8: 16, E4M3: 16, INT4: 32}.get(cache_format)
+            if unit is None:
+                raise ValueError("cache_format is INT8, E4M3 or INT4")
+            if problem.head_dim % unit or problem.head_dim > 256:
+                raise ValueError(f"a cache of this format holds heads of a multiple of {unit} channels, up to 256")
         self.page_size = int(page_size)
         unit = max(self.page_size, 1)
         p = self.problem = problem
@@ -570,7 +578,12 @@ class CompressionPass:
         torch.eq(page, last, out=hit)
         torch.where(hit, fewer, full, out=self.row_count.view(-1))
 
+    def _check_holds_cache(self):
+        if self.k_out is None:
+            raise ValueError("the pass was made without a reduced cache (cache_dtype or cache_format, with_cache)")
+
     def compact(self, k_cache, v_cache):
+        self._check_holds_cache()
         if self.cache_format is not None:
             kvcrush_quantize(self.problem, k_cache, v_cache, self.k_out, self.v_out, cu_kept=self.cu_kept, idx=self.idx,
                              total_kept=self.total_kept, out_begin=self.row_begin, status=self.status)
@@ -583,6 +596,8 @@ class CompressionPass:
                         self.v_out, status=self.status)
 
     def run(self, q, k, k_cache=None, v_cache=None, lse_in=None):
+        if k_cache is not None:
+            self._check_holds_cache()                     # before the first stage is enqueued
         self.score(q, k, lse_in)
         if self.pooled is not None:
             self.pool()
