@@ -384,7 +384,10 @@ int kvcrush_signature_static(const kvcrush_problem_t* problem, const float* scor
  *   INT8   value = scale * code             code in -127 .. 127, scale = max|x| * (1/127)
  *   E4M3   value = scale * code             code an 8-bit float (4 exponent, 3 mantissa bits), scale = max|x| * (1/448)
  *   INT4   value = zero + scale * code      code in 0 .. 15, zero = min x, scale = (max x - min x) * (1/15)
- * Codes are the quotient x / scale (INT4: (x - zero) / scale), rounded to the nearest code, ties to even.  A scale below
+ * Codes are the quotient x * 127 / max|x|, x * 448 / max|x| or (x - min x) * 15 / (max x - min x), rounded to the nearest code, ties
+ * to even.  Exactly so for rows of BF16 and FP16, but in INT4 rows whose min x or max x is not zero and less than 2^-7 of
+ * max x - min x: there, and in FP32 rows, a quotient that lies within 2^-18 (FP32: 2^-21 of its size) of the border between two codes may
+ * get either (and INT4 takes values below 2^-80 for zero beside a span above 2^64).  A scale below
  * the smallest normal float32 is stored as 0 and so are the row's codes.  A row that holds an infinity or a NaN (INT4:
  * also one whose span overflows) gets NaN as its scale and zero, and codes 0: it reads back as NaN throughout.
  * Strides of INT4 codes count channels; like every other stride they must come to multiples of 16 bytes.
