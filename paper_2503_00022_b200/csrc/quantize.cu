@@ -81,7 +81,7 @@ __device__ __forceinline__ float side(float x) {
 __device__ __forceinline__ void codes_by_borders(const float (&x)[8], float lo, float hi, float shift, float inv, uint32_t (&c)[8]) {
   const tc::f32x2 magic = tc::splat2(12582912.f), minus_magic = tc::splat2(-12582912.f);     // as in quantize_row
   const tc::f32x2 factor = tc::splat2(15.f * shift * inv), first = tc::splat2(fmaf(-lo, 15.f * shift * inv, -0.5f)), num = tc::splat2(15.f * shift);
-  const tc::f32x2 step = tc::splat2((lo - hi) * shift), start = tc::splat2(fmaf(-14.5f, lo, -0.5f * hi) * shift);
+  const tc::f32x2 step = tc::splat2((lo - hi) * shift), start = tc::splat2(fmaf(-14.5f, lo * shift, -0.5f * (hi * shift)));
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
     const tc::f32x2 y = tc::pack2f(x[i], x[i + 1]);

@@ -110,3 +110,17 @@ def test_four_bit_rows_whose_middle_is_not_quite_the_middle(B, dtype):
         assert codes[0] == 0 | 15 << 4 and codes[1] & 15 in (7, 8) and codes[1] >> 4 in (7, 8) and codes[2] == 8 | 8 << 4
     else:
         assert codes == [0 | 15 << 4, 7 | 8 << 4, 8 | 8 << 4]
+
+
+@pytest.mark.parametrize("power", [-80, 118])
+@pytest.mark.parametrize("fmt", [C.INT8, C.E4M3, C.INT4])
+def test_the_same_codes_near_the_ends_of_the_range(B, fmt, power):
+    """The rows of the test above in bf16 times a power of two: the quotients, and so the codes, are the same numbers."""
+    import torch
+    D = 64
+    rows = _rows("bf16", fmt, D)
+    x = torch.from_numpy(rows * 2.0 ** power).to("cuda:0").to(torch.bfloat16).view(1, -1, 1, D)
+    assert np.array_equal(TL.numpy64(x)[0, :, 0], rows * 2.0 ** power)
+    got, plain = (TL.quantise(B, t, fmt)[0] for t in (x, torch.from_numpy(rows).to("cuda:0").to(torch.bfloat16).view(1, -1, 1, D)))
+    assert torch.equal(got.codes, plain.codes)
+    assert np.array_equal(got.scales.double().cpu().numpy(), plain.scales.double().cpu().numpy() * 2.0 ** power)
