@@ -445,8 +445,9 @@ __device__ __forceinline__ void join_and_write(const AttendArgs& a, const Unit& 
       sum.x += v.x == 0.f ? 0.f : v.x * f2; sum.y += v.y == 0.f ? 0.f : v.y * f2;
       sum.z += v.z == 0.f ? 0.f : v.z * f2; sum.w += v.w == 0.f ? 0.f : v.w * f2;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const float x[4] = {(sum.x + b) * inv, (sum.y + b) * inv, (sum.z + b) * inv, (sum.w + b) * inv};
+    const bool none = l == 0.f;                        // no weight: zeros, whatever the values hold (0 times infinity)
+    const float inv = 1.f / l;
+    const float x[4] = {none ? 0.f : (sum.x + b) * inv, none ? 0.f : (sum.y + b) * inv, none ? 0.f : (sum.z + b) * inv, none ? 0.f : (sum.w + b) * inv};
     const int token = w.token(row), head = w.hk * w.G + row + w.row0 - token * w.G;
     unsigned char* op = static_cast<unsigned char*>(const_cast<void*>(a.O.ptr)) +
         bytes_of<FQ>(w.layer * a.O.sl + (w.first + token) * a.O.st + head * a.O.sh + d);

@@ -520,12 +520,14 @@ attend_tree_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       sum_l = fmaf(q.y, f, sum_l);
       sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
     }
-    const float inv = sum_l == 0.f ? 0.f : 1.f / sum_l;
+    const bool none = sum_l == 0.f;                    // no weight: zeros, whatever the values hold (0 times infinity)
+    const float inv = 1.f / sum_l;
+    const float x[4] = {none ? 0.f : sum.x * inv, none ? 0.f : sum.y * inv, none ? 0.f : sum.z * inv, none ? 0.f : sum.w * inv};
     const int token = w.token(row), head = w.hk * w.G + row + w.row0 - token * w.G;
     unsigned char* op = static_cast<unsigned char*>(const_cast<void*>(a.O.ptr)) +
         bytes_of<FQ>(w.layer * a.O.sl + (w.first + token) * a.O.st + head * a.O.sh + d);
-    if constexpr (FQ == KVCRUSH_BF16) *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
-    else *reinterpret_cast<uint2*>(op) = make_uint2(pack_fp16(sum.x * inv, sum.y * inv), pack_fp16(sum.z * inv, sum.w * inv));
+    if constexpr (FQ == KVCRUSH_BF16) *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+    else *reinterpret_cast<uint2*>(op) = make_uint2(pack_fp16(x[0], x[1]), pack_fp16(x[2], x[3]));
     if (d == 0 && a.lse)
       a.lse[((long long)w.layer * s.Hq + head) * a.fresh.total + w.first + token] = sum_l == 0.f ? neg_inf() : (top + log2f(sum_l)) * 0.6931471805599453f;
   }
