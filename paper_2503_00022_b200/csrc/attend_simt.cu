@@ -253,9 +253,13 @@ int launch_one(AttendArgs& a, cudaStream_t stream) {
   auto kern = attend_simt_kernel<FQ, F, kPages>;
   const Shape& s = a.s;
   const size_t dyn = kOBytes + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
-  static ClusterTable table;
   const int bound = kOBytes + (kPages ? (int)page_mem_bytes(kMaxPagesPerSeq, kMaxPagesPerSeq, kMaxD) : 0);
-  const std::atomic<int>* resident = table.resident(kern, kWarps * 32, bound, bound);
+  // One table for launches that leave room for two blocks an SM, one for those with many pages.  64 pages of 32 out of 1024, 8 KV heads
+  // of 128 with 4 query heads each: 57 us (96 with every launch planned as if it took the room of 8192 pages).
+  static ClusterTable table, large;
+  constexpr int kStatic = kRows * kMaxD * 4 + kWarps * kTile * kRows * 4 + kWarps * kRows * (int)sizeof(Part) + (int)sizeof(Received<kRows, kMaxD>);
+  const int two = bound < 113 * 1024 - kStatic ? bound : 113 * 1024 - kStatic;
+  const std::atomic<int>* resident = dyn <= (size_t)two ? table.resident(kern, kWarps * 32, two, bound) : large.resident(kern, kWarps * 32, bound, bound);
   if (!resident) return KVCRUSH_ERR_CUDA;
   const int n_blk = choose_cluster(resident, attend_units(a, kRows), attend_tiles(a), 2 * kWarps);
   dim3 grid;
