@@ -16,18 +16,15 @@ using namespace fmt;
 constexpr int kWarps = 4;
 constexpr int kRows = 8;                     // query rows of a unit
 constexpr int kMaxD = 256;
+constexpr int FQ = KVCRUSH_FP32;            // queries, new tokens and bounds of pages
 constexpr int kOBytes = kWarps * kRows * kMaxD * 4;
 
-// Four consecutive channels: values, or codes.
+// Four consecutive channels: float32 values, or codes.
 template <int F>
 __device__ __forceinline__ void load4(const unsigned char* p, float (&x)[4]) {
   if constexpr (F == KVCRUSH_FP32) {
     const float4 v = __ldcs(reinterpret_cast<const float4*>(p));
     x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-  } else if constexpr (F == KVCRUSH_BF16 || F == KVCRUSH_FP16) {
-    const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p));
-    const float2 a = F == KVCRUSH_BF16 ? unpack_bf16(v.x) : unpack_fp16(v.x), b = F == KVCRUSH_BF16 ? unpack_bf16(v.y) : unpack_fp16(v.y);
-    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
   } else if constexpr (F == KVCRUSH_INT4) {
     codes4<F>(__ldcs(reinterpret_cast<const unsigned short*>(p)), x);
   } else {
@@ -153,7 +150,7 @@ __device__ __forceinline__ void tile(const CacheView& K, const CacheView& V, lon
   }
 }
 
-template <int FQ, int F, bool kPages>
+template <int F, bool kPages>
 __global__ void __launch_bounds__(kWarps * 32)
 attend_simt_kernel(AttendArgs a) {
   extern __shared__ __align__(16) unsigned char dyn_sh[];            // outputs of the warps, then what the choice of pages needs
@@ -248,9 +245,9 @@ attend_simt_kernel(AttendArgs a) {
   join_and_write<FQ, kWarps, kRows, kMaxD>(a, w, cluster, n_blk, rank, o, kMaxD, warp_part[0], &recv);
 }
 
-template <int FQ, int F, bool kPages>
+template <int F, bool kPages>
 int launch_one(AttendArgs& a, cudaStream_t stream) {
-  auto kern = attend_simt_kernel<FQ, F, kPages>;
+  auto kern = attend_simt_kernel<F, kPages>;
   const Shape& s = a.s;
   const size_t dyn = kOBytes + (kPages ? page_mem_bytes(a.pages.max_pages, a.pages.budget, s.D) : 0);
   const int bound = kOBytes + (kPages ? (int)page_mem_bytes(kMaxPagesPerSeq, kMaxPagesPerSeq, kMaxD) : 0);
@@ -267,23 +264,20 @@ int launch_one(AttendArgs& a, cudaStream_t stream) {
   return launch_chained(kern, grid, dim3(kWarps * 32), dyn, stream, n_blk, a);
 }
 
-template <int FQ, int F>
+template <int F>
 int launch_pages(AttendArgs& a, cudaStream_t stream) {
-  return a.pages.page_size ? launch_one<FQ, F, true>(a, stream) : launch_one<FQ, F, false>(a, stream);
-}
-
-template <int FQ>
-int launch_formats(AttendArgs& a, cudaStream_t stream) {
-  switch (a.K.dtype) {
-    case KVCRUSH_INT8: return launch_pages<FQ, KVCRUSH_INT8>(a, stream);
-    case KVCRUSH_E4M3: return launch_pages<FQ, KVCRUSH_E4M3>(a, stream);
-    case KVCRUSH_INT4: return launch_pages<FQ, KVCRUSH_INT4>(a, stream);
-    default: return launch_pages<FQ, FQ>(a, stream);
-  }
+  return a.pages.page_size ? launch_one<F, true>(a, stream) : launch_one<F, false>(a, stream);
 }
 
 }  // namespace
 
-int launch_attend_simt(AttendArgs a, cudaStream_t stream) { return launch_formats<KVCRUSH_FP32>(a, stream); }
+int launch_attend_simt(AttendArgs a, cudaStream_t stream) {
+  switch (a.K.dtype) {
+    case KVCRUSH_INT8: return launch_pages<KVCRUSH_INT8>(a, stream);
+    case KVCRUSH_E4M3: return launch_pages<KVCRUSH_E4M3>(a, stream);
+    case KVCRUSH_INT4: return launch_pages<KVCRUSH_INT4>(a, stream);
+    default: return launch_pages<KVCRUSH_FP32>(a, stream);
+  }
+}
 
 }  // namespace kvc
