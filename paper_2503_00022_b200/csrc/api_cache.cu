@@ -14,6 +14,10 @@ constexpr int kMaxPageSize = 1024;
 constexpr uint32_t kWaitPolls = 1u << 20, kShortWaitPolls = 1u << 12;   // limits of a barrier wait
 constexpr long long kMaxStep = 1LL << 31;            // bytes from one token to the next, in the attention kernels
 
+// Is it that far from one token to the next?  stride: in elements of `bits`.
+bool too_far(long long stride, int bits) { return stride >= kMaxStep * 8 / bits; }
+int element_bits(int dtype) { return dtype == KVCRUSH_INT4 ? 4 : dtype == KVCRUSH_INT8 || dtype == KVCRUSH_E4M3 ? 8 : 8 * elt_bytes(dtype); }
+
 // A tensor that nothing is read from or written to may have no memory.
 alignas(16) const unsigned char kNowhere[16] = {};
 int make_view(const kvcrush_tensor_t* t, int head_dim, bool empty, TensorView* v) {
@@ -121,8 +125,8 @@ int make_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* ne
   if ((rc = make_cache(K, K_scales, s.D, s.T == 0, &a->K)) != KVCRUSH_OK) return rc;
   if ((rc = make_cache(V, V_scales, s.D, s.T == 0, &a->V)) != KVCRUSH_OK) return rc;
   if (a->O.dtype != a->Q.dtype || a->K.dtype != a->V.dtype || (!K_scales && a->K.dtype != a->Q.dtype)) return KVCRUSH_ERR_INVALID_ARG;
-  const int eb = elt_bytes(a->Q.dtype);
-  if (a->K.st * eb >= kMaxStep || a->V.st * eb >= kMaxStep || a->K.sct * 4 >= kMaxStep || a->V.sct * 4 >= kMaxStep) return KVCRUSH_ERR_UNSUPPORTED;
+  const int bits = element_bits(a->K.dtype);
+  if (too_far(a->K.st, bits) || too_far(a->V.st, bits) || too_far(a->K.sct, 32) || too_far(a->V.sct, 32)) return KVCRUSH_ERR_UNSUPPORTED;
   a->group_magic = s.G > 1 ? 0xFFFFFFFFu / (uint32_t)s.G + 1u : 0u;
   a->row_begin = row_begin_dev;
   a->row_count = row_count_dev;
@@ -193,8 +197,8 @@ int attend_entry(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* n
   if (K_new) {
     if ((rc = view_from_tensor(K_new, a.s.D, &a.K_new)) != KVCRUSH_OK) return rc;
     if ((rc = view_from_tensor(V_new, a.s.D, &a.V_new)) != KVCRUSH_OK) return rc;
-    if (a.K_new.st * elt_bytes(a.Q.dtype) >= kMaxStep || a.V_new.st * elt_bytes(a.Q.dtype) >= kMaxStep) return KVCRUSH_ERR_UNSUPPORTED;
     if (a.K_new.dtype != a.Q.dtype || a.V_new.dtype != a.Q.dtype) return KVCRUSH_ERR_INVALID_ARG;
+    if (too_far(a.K_new.st, element_bits(a.Q.dtype)) || too_far(a.V_new.st, element_bits(a.Q.dtype))) return KVCRUSH_ERR_UNSUPPORTED;
   }
   if (short_waits) a.polls = kShortWaitPolls;
   a.withhold = withhold;
