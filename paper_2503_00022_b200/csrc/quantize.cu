@@ -6,8 +6,9 @@
 // largest value) is found by shuffles while the row stays in registers.
 //
 // 32 layers x 2048 rows x 32 heads of 128, both tensors: bf16 to 8 bits 278 us = 5.8 TB/s
-// (591 with a row to 16 lanes, one row a warp and unpaired arithmetic), to 4 bits 298; back 261 = 6.2 TB/s and 235.  What keeps
-// the way in below the way out is arithmetic: about 12.6 instructions a value, the ALU pipe busy for 54 %.
+// (591 with a row to 16 lanes, one row a warp and unpaired arithmetic), to 4 bits 319 = 4.3 TB/s; back 257 = 6.3 TB/s and 233.  What keeps
+// the way in below the way out is arithmetic: about 12.6 instructions a value to 8 bits, 17 to 4 bits (301 us with codes that are not
+// always the nearest, see below); issue slots are 71 % busy there, DRAM 38 %.
 //
 // Codes are quotients rounded to the nearest code.  Rows of 16-bit values have few significant bits, so that quotients often
 // lie on the border between two codes exactly, and a product with a rounded reciprocal would fall on either side.  The
@@ -70,7 +71,6 @@ __device__ __forceinline__ float least3(float a, float b, float c) {
 // The bracket is exact where both ends are zero or at least 2^-7 of the span: multiples of half the smaller end's last place, less
 // than 2^24 of them.  r is then one rounding of the exact value, which keeps its sign.  Where an end is smaller, the bracket is off by
 // 2^-18 of the span at most (half steps of float32: 14.5 and 15 for its constants, 15 for itself), and so is the quotient that decides.
-// It costs 10 % of the way in against the quotient's remainder alone (32 heads of 128 in bf16, 403 MB: 86 -> 95 us).
 // 0, 1/2 or 1 for a negative, zero or positive x
 __device__ __forceinline__ float side(float x) {
   float d;
@@ -293,7 +293,9 @@ convert_kernel(Shape s, ConvertArgs a, int n_tensors) {
 
 template <int FI, int FO, int kLanes, int kVecs>
 int launch_lanes(const Shape& s, ConvertArgs& a, int n_tensors, cudaStream_t stream) {
-  constexpr int kSteps = kVecs == 1 ? 4 : kVecs == 2 ? 2 : 1, heads = kSteps * 32 / kLanes;
+  // Half as many rows in flight on the way to 4 bits, whose constants need the registers: with as many as elsewhere, and spills, 32
+  // heads of 128 took 173 us for 157, heads of 64 123 for 66.
+  constexpr int kInFlight = FO == KVCRUSH_INT4 ? 2 : 4, kSteps = kVecs == 1 ? kInFlight : kVecs == 2 ? kInFlight / 2 : 1, heads = kSteps * 32 / kLanes;
   a.chunks = (s.Hkv + heads - 1) / heads;
   // as many rows a warp as leave the chip several times the warps it holds
   a.rows_per_warp = 1;
