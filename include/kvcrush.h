@@ -416,7 +416,8 @@ typedef struct kvcrush_scales {
  *                  16- or 32-bit side: BF16, FP16 or FP32.  head_dim <= 256, a multiple of 8; INT8 and E4M3: of 16,
  *                  INT4: of 32
  * Tensors and scales may have NULL pointers where there is no row (total_kept 0, or no list and no token).
- * Rows that the lists do not name are left as they were.  Two rows written to one place are a race.
+ * Rows that the lists do not name are left as they were.  Two rows written to one place are a race.  That every row named exists,
+ * where it is read and where it is written, is the caller's to see to (a cache that is full takes no more rows).
  */
 int kvcrush_quantize(const kvcrush_problem_t* problem, const kvcrush_tensor_t* K, const kvcrush_tensor_t* V,
                      const int32_t* cu_kept_dev, const int32_t* idx_dev, int64_t total_kept,
@@ -453,7 +454,8 @@ typedef struct kvcrush_new_tokens {
  *                  causal and query_window are ignored
  *   row_begin_dev, optional [n_layers][n_seqs] int32, both or none: where each sequence's rows start in its layer, and how
  *   row_count_dev  many there are (reduced caches differ from layer to layer; a cache grows while it is used).  Counts are
- *                  taken up to max_seqlen and up to the layer's end.  NULL: cu_seqlens
+ *                  taken up to max_seqlen and up to the layer's end.  NULL: cu_seqlens.  Every row counted is a key: the zeros
+ *                  that kvcrush_compact_pages writes behind a short last page are left out of the count by the caller
  *   Q, K_new, V_new, O   [n_layers][total_new][heads][head_dim]; Q, K_new, V_new and O are of one type, BF16, FP16 or
  *                  FP32; K_new and V_new both or none
  *   K, V           the cache: of Q's type (scales NULL) or quantised, both in the same type
@@ -462,7 +464,10 @@ typedef struct kvcrush_new_tokens {
  * bytes from a token to the next.  Without new tokens (total_new 0) nothing is done; K and V of a problem without rows may have NULL pointers.  A token that sees no row, or whose logits are
  * all -inf, gets zeros and a log-sum-exp of -inf.  Rows that a token does not see have no influence on its output,
  * whatever they hold.  Logits, softmax statistics and sums are float32; the weights are rounded to the 16-bit type that
- * they are multiplied in (FP32: not at all).  Results do not depend on what else runs, nor on the order of the blocks.
+ * they are multiplied in (FP32 queries: not at all): Q's, and FP16 for the rows of a quantised cache.  In FP16 weights below 2^-25 of
+ * a row's largest vanish from the output, not from the log-sum-exp.  Queries over a quantised cache are multiplied in FP16 too, times
+ * a power of two for each row: BF16 values keep their bits but for those 2^-25 below the row's largest.  (BF16 queries over INT8 and INT4
+ * caches: less than 2^110 in magnitude.)  Results do not depend on what else runs, nor on the order of the blocks.
  */
 int kvcrush_attend(const kvcrush_problem_t* problem, const kvcrush_new_tokens_t* new_tokens, const kvcrush_tensor_t* Q,
                    const kvcrush_tensor_t* K, const kvcrush_scales_t* K_scales,
@@ -496,7 +501,8 @@ int kvcrush_page_bounds(const kvcrush_problem_t* problem, const kvcrush_tensor_t
  * are left out, a NaN counts as +inf).
  * The first keep_initial and the last keep_recent pages come before all others (lower page first), then pages by
  * score (ties: lower page); the first `budget` of this order are attended to, or all of them if there are fewer.
- *   lo, hi         as kvcrush_page_bounds writes them, of Q's type; total rows n_seqs * max_pages
+ *   lo, hi         as kvcrush_page_bounds writes them, of Q's type; total rows n_seqs * max_pages.  Over a quantised cache they are
+ *                  the bounds of the keys before they were rounded to codes
  *   budget         >= 1
  *   page_idx_dev   optional out [n_layers][total_new][n_kv_heads][budget] int32: the pages, ascending, then -1
  *   n_pages_dev    optional out [n_layers][total_new][n_kv_heads] int32: how many there are

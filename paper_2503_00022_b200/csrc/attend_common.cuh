@@ -497,7 +497,8 @@ struct ClusterTable {
   }
 };
 // Blocks for each of `units` units of `tiles` tiles: the fewest rounds of resident clusters times what a block takes, its tiles and
-// `fixed` tiles' worth of what it does once.
+// `fixed` tiles' worth of what it does once.  How many is of little account: from 0 to 20 tiles a warp (attend_tree.cu: a block) thirteen
+// calls of one to 63 tokens over 1001 to 48000 rows, of all three kernels and over pages, took the same time to 1 %.
 inline int choose_cluster(const std::atomic<int>* resident, long long units, int tiles, int fixed) {
   int best = 1;
   long long best_cost = -1;

@@ -16,6 +16,10 @@
 // 300 instructions and 1400 to 1700 clocks for 4-bit codes, 208 instructions for 16-bit values, at 7 to 8 warps an SM) and by what a block
 // does once: 750 to 1000 clocks to find its unit, 1000 to 5000 for queries and first tiles, 2800 to 10000 for the join, which
 // waits for the slowest block.
+// Blocks of 32 rows over codes spill (128 channels: 488 bytes for 4-bit codes, 392 and 68 for 8-bit ones, at 255 registers), and so do
+// those of 16 rows of 64 channels with eight warps (56 to 104 bytes at 128).  Many rows over codes are slow for that and because every
+// block unpacks the cache again: 63 tokens of the heads above over 32768 rows take 309 us in INT8, 198 in E4M3, 281 in INT4, where
+// bf16 goes through attend_tree.cu in 63; 15 tokens 110, 71 and 100 for 42.
 #pragma once
 
 #include "attend_common.cuh"

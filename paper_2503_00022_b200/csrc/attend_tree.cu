@@ -550,8 +550,17 @@ int launch_one(const AttendArgs& a, const CUtensorMap (&maps)[4], cudaStream_t s
 
 }  // namespace
 
-// From more than 16 query rows on (20 rows over 32768: 40 us against 45; up to 16 attend_mma.cuh reads the cache once at HBM's
-// pace) and two tiles of keys; a negative scale would turn the maximum around.
+// From more than 16 query rows on, and two tiles of keys; a negative scale would turn the maximum around.  us of this kernel / of
+// attend_mma.cuh (whose blocks take 8, 16 or 32 rows), bf16, caches out of HBM:
+//   KV heads x channels, cached rows      16 rows      20 rows      40 rows
+//   8 x 128, 2048                        11.0 / 9.6   11.0 / 11.7  11.8 / 13.3
+//   8 x 128, 32768                       40.4 / 33.0  40.5 / 45.3  41.0 / 53.6
+//   8 x 64, 32768                        33.7 / 21.2  33.8 / 28.6  33.8 / 33.4
+//   32 x 128, 32768                      92.9 / 82.4  92.0 / 87.2  93.9 / 157
+//   32 x 64, 32768                       72.1 / 53.0  72.3 / 49.6  72.2 / 85.6
+//   32 x 128, 16 sequences of 2048        124 / 91.0   125 / 100    133 / 210
+// So up to 16 rows the other one is ahead everywhere and from 33 on nearly everywhere this one; between, this one is ahead for few
+// heads of 128 over long caches only, and the rule, which does not look at heads and channels, costs the others up to a third.
 bool attend_tree_fits(const AttendArgs& a) {
   const long long rows = (long long)a.fresh.most * a.s.G;
   return a.pages.page_size == 0 && (a.K.dtype == KVCRUSH_BF16 || a.K.dtype == KVCRUSH_FP16) && a.s.D <= 128 && rows > 16 &&
