@@ -2,7 +2,8 @@
 
 Only argument marshalling lives here.  torch is used to own device memory and to
 name the CUDA stream; every step of the compression pass runs inside the library's
-kernels.  There is no CPU fallback: if the library cannot be loaded the first call
+kernels (a pass over pages counts the rows of its reduced cache with three torch operations
+where the selection decides them).  There is no CPU fallback: if the library cannot be loaded the first call
 raises.
 """
 from __future__ import annotations

@@ -8,7 +8,7 @@
 // 32 layers x 2048 rows x 32 heads of 128, both tensors: bf16 to 8 bits 278 us = 5.8 TB/s
 // (591 with a row to 16 lanes, one row a warp and unpaired arithmetic), to 4 bits 319 = 4.3 TB/s; back 257 = 6.3 TB/s and 233.  What keeps
 // the way in below the way out is arithmetic: about 12.6 instructions a value to 8 bits, 17 to 4 bits (301 us with codes that are not
-// always the nearest, see below); issue slots are 71 % busy there, DRAM 38 %.
+// always the nearest, see below); issue slots are 72 % busy there, DRAM 41 %.
 //
 // Codes are quotients rounded to the nearest code.  Rows of 16-bit values have few significant bits, so that quotients often
 // lie on the border between two codes exactly, and a product with a rounded reciprocal would fall on either side.  The
