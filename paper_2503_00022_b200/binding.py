@@ -435,7 +435,7 @@ class CompressionPass:
     page_size > 0 selects and gathers whole pages of that many tokens: budgets then count pages,
     ``idx`` holds page numbers, the reduced cache has page_size rows per kept page and keep_initial /
     keep_recent count pages as well.  ``row_count`` leaves out the slots of a short last page that hold no token; it is
-    current from ``select`` on.
+    current once ``compact`` has been called.
 
     cache_format INT8, E4M3 or INT4 (kept tokens, not pages) quantises the reduced cache as it is written: ``k_out`` and
     ``v_out`` are then QuantTensors.  spare_rows leaves room behind each sequence's kept rows, so that new tokens can be
@@ -560,7 +560,6 @@ class CompressionPass:
                                  n_kept=self.n_kept, anchor_mode=self.anchor_mode, anchor_bits=self.anchor_bits,
                                  keep_initial=self.keep_initial, keep_recent=self.keep_recent,
                                  workspace=self.workspace, status=self.status)
-            self._count_rows()
             return
         kvcrush_select(self.problem, sc, self.sigs, self.budget_imp,
                        self.budget_rep, self.cu_kept, self.idx, importance=imp, kind=self.kind, n_kept=self.n_kept,
@@ -592,6 +591,7 @@ class CompressionPass:
         if self.page_size:
             kvcrush_compact_pages(self.problem, k_cache, v_cache, self.page_size, self.cu_kept, self.idx,
                                   self.total_kept, self.k_out, self.v_out, status=self.status)
+            self._count_rows()
             return
         kvcrush_compact(self.problem, k_cache, v_cache, self.cu_kept, self.idx, self.total_kept, self.k_out,
                         self.v_out, status=self.status)

@@ -124,3 +124,33 @@ def test_the_same_codes_near_the_ends_of_the_range(B, fmt, power):
     got, plain = (TL.quantise(B, t, fmt)[0] for t in (x, torch.from_numpy(rows).to("cuda:0").to(torch.bfloat16).view(1, -1, 1, D)))
     assert torch.equal(got.codes, plain.codes)
     assert np.array_equal(got.scales.double().cpu().numpy(), plain.scales.double().cpu().numpy() * 2.0 ** power)
+
+
+@pytest.mark.parametrize("fmt", [C.INT8, C.E4M3, C.INT4])
+@pytest.mark.parametrize("dtype,most", [("bf16", 255), ("fp16", 2047)])
+def test_rows_of_whole_numbers(B, dtype, fmt, most):
+    """Whole numbers around a middle, near 0 and far from it: spans of a few units to most of the type's whole numbers, many ties."""
+    import torch
+    g = np.random.Generator(np.random.Philox(790 + fmt))
+    n, D = 4000, 64
+    width = np.exp2(g.uniform(0.5, np.log2(most), (n, 1))).astype(int)
+    middle = g.integers(-most, most + 1, (n, 1)) * g.integers(0, 2, (n, 1))
+    rows = np.clip(middle + g.integers(-width, width + 1, (n, D)), -most, most).astype(np.float64)
+    x = torch.from_numpy(rows).to("cuda:0").to(TL.torch_dtype(dtype)).view(1, n, 1, D)
+    assert np.array_equal(TL.numpy64(x)[0, :, 0], rows)
+    q, _ = TL.quantise(B, x, fmt)
+    y = C.quotients(rows, fmt)[0]
+    scales = q.scales.cpu().numpy()
+    plain = np.stack([np.ones(scales.shape[:3]), np.zeros(scales.shape[:3])], -1) if fmt == C.INT4 else np.ones_like(scales)
+    got = C.decode(q.codes.cpu().numpy(), plain, fmt)[0, :, 0]
+    want = C.round_e4m3(y) if fmt == C.E4M3 else np.rint(y)
+    # ends that are not zero are 2^-7 of the span or more but for the longest rows of float16 (1 beside 4094)
+    near = np.zeros((n, 1))
+    if fmt == C.INT4:
+        ends, span = np.abs(np.stack([rows.min(-1), rows.max(-1)], -1)), rows.max(-1) - rows.min(-1)
+        near = np.where(((ends > 0) & (ends < 2.0 ** -7 * span[:, None])).any(-1), 2.0 ** -18, 0.0)[:, None]
+        assert (near == 0).mean() > 0.9
+    bad = np.argwhere((got != want) & (np.abs(y - (got + want) / 2) > near))
+    assert len(bad) == 0, [(rows[b[0]].min(), rows[b[0]].max(), rows[tuple(b)], y[tuple(b)], got[tuple(b)]) for b in bad[:5]]
+    if fmt != C.E4M3:
+        assert (np.abs(y - np.trunc(y)) == 0.5).sum() > 100
