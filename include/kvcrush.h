@@ -464,8 +464,9 @@ typedef struct kvcrush_new_tokens {
  * bytes from a token to the next.  Without new tokens (total_new 0) nothing is done; K and V of a problem without rows may have NULL pointers.  A token that sees no row, or whose logits are
  * all -inf, gets zeros and a log-sum-exp of -inf.  Rows that a token does not see have no influence on its output,
  * whatever they hold.  Logits, softmax statistics and sums are float32; the weights are rounded to the 16-bit type that
- * they are multiplied in (FP32 queries: not at all): Q's, and FP16 for the rows of a quantised cache.  In FP16 weights below 2^-25 of
- * a row's largest vanish from the output, not from the log-sum-exp.  Queries over a quantised cache are multiplied in FP16 too, times
+ * they are multiplied in (FP32 queries: not at all): Q's, and FP16 for the rows of a quantised cache, where a weight times the row's
+ * scale multiplies the row's codes: errors are in proportion to the rows' scales, not to what a channel holds.  In FP16 weights below
+ * 2^-25 of a row's largest vanish from the output, not from the log-sum-exp.  Queries over a quantised cache are multiplied in FP16 too, times
  * a power of two for each row: BF16 values keep their bits but for those 2^-25 below the row's largest.  (BF16 queries over INT8 and INT4
  * caches: less than 2^110 in magnitude.)  Results do not depend on what else runs, nor on the order of the blocks.
  */
